@@ -203,6 +203,73 @@ sla_status_t sla_fp8_linear_qkv(const void *x, const void *W, const void *bias, 
                                 void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Norm of every head's queries and keys and position rotation, in one pass from a projection's output to the form the
+ * attention takes its inputs in.  For every token and head, over the 64 channels of its row x of q (and of k):
+ *     u = (x - m) r,  r = 1 / sqrt(mean((x - m)^2) + eps)      m = mean(x) (SLA_NORM_LAYER), 0 (SLA_NORM_RMS)
+ *     n = u * weight + bias                                    (SLA_NORM_NONE: n = x)
+ *     y_i = n_i cos a - n_p sin a,   y_p = n_p cos a + n_i sin a      for each pair (i, p) of channels
+ * Rotation: axes = 1: one position per token turns all 64 channels, pair j = 0 .. 31 by a = position * base^(-j / 32);
+ * axes = 2: two positions (row and column of a patch) turn channels 0 .. 31 and 32 .. 63, pair j = 0 .. 15 of each half by
+ * a = position * base^(-j / 16); axes = 0: none.  The pairs of a span of S channels are (j, j + S/2) (SLA_PAIR_HALVES)
+ * or (2j, 2j + 1) (SLA_PAIR_ADJACENT).  Angles are reduced in 64 bits: any int32 position is as exact as a small one.
+ * v rows are brought into the output layout (and data type) unchanged.
+ */
+typedef enum { SLA_NORM_NONE = 0, SLA_NORM_RMS = 1, SLA_NORM_LAYER = 2 } sla_norm_t;
+typedef enum { SLA_PAIR_HALVES = 0, SLA_PAIR_ADJACENT = 1 } sla_pairing_t;
+
+typedef struct {
+    int32_t B, H, N, D;          /* batch, heads, tokens per item, head dim (must be 64) */
+    int32_t norm;                /* sla_norm_t */
+    int32_t norm_per_head;       /* weights and biases: 0: [D]; 1: [H, D] */
+    int32_t axes;                /* positions per token: 0 (no rotation), 1 or 2 */
+    int32_t pairing;             /* sla_pairing_t */
+    int32_t pos_per_item;        /* positions: 0: [N, axes], the same for every item; 1: [B, N, axes] */
+    int32_t layout;              /* sla_layout_t of the outputs Q, K, V (and of dQ, dK, dV) */
+    float   eps;                 /* > 0 unless SLA_NORM_NONE; the squares are summed in fp32, so |x| must stay below 2^60 */
+    double  base;                /* >= 1, finite; ignored with axes = 0 */
+    int64_t batch_stride, token_stride, head_stride;
+                                 /* elements between the rows of q, k, v (and of dq, dk, dv): multiples of 8, at least 64, and
+                                    no two rows overlap.  A fused projection [B,N,3,H,64]: N 3 H 64, 3 H 64, 64 */
+} sla_heads_params_t;
+
+/*
+ *   q, k, v         in   bf16, a row of 64 at b batch_stride + t token_stride + h head_stride; v may be NULL (and V with it)
+ *   *_weight, *_bias in  fp32 [D] or [H, D], each may be NULL (1 and 0); all NULL with SLA_NORM_NONE
+ *   pos             in   int32, see pos_per_item; NULL with axes = 0
+ *   Q, K, V         out  bf16 in `layout`
+ */
+sla_status_t sla_qk_norm_rope(const sla_heads_params_t *p, const void *q, const void *k, const void *v,
+                              const float *q_weight, const float *q_bias, const float *k_weight, const float *k_bias,
+                              const int32_t *pos, void *Q, void *K, void *V, void *stream);
+
+/*
+ * The same with the outputs in the E4M3 form that sla_forward takes: codes in `layout` and block scales as
+ * sla_quantise_e4m3 defines them (blk = bq for Q, 64 for K and V; scale = max(amax, 1e-8) / 448), of the values y before any
+ * rounding to bf16: one rounding, to E4M3.  V comes out as sla_quantise_e4m3 would leave it, bit for bit.
+ *   Q8, K8, V8  out  uint8;   sQ  out  fp32 [B,H,ceil(N/bq)];   sK, sV  out  fp32 [B,H,ceil(N/64)]
+ */
+sla_status_t sla_qk_norm_rope_e4m3(const sla_heads_params_t *p, const void *q, const void *k, const void *v,
+                                   const float *q_weight, const float *q_bias, const float *k_weight, const float *k_bias,
+                                   const int32_t *pos, int32_t bq, void *Q8, void *K8, void *V8, float *sQ, float *sK, float *sV,
+                                   void *stream);
+
+/*
+ * Gradients of sla_qk_norm_rope (and, straight through the quantiser, of the E4M3 form).
+ *   q, k, weights, pos   in   as in the forward
+ *   dQ, dK, dV           in   bf16 in `layout`, gradients of Q, K, V; dV NULL exactly if dv is
+ *   dq, dk, dv           out  bf16 in the strides of q, k, v (the three slices of one [B,N,3,H,64] tensor, say); elements between
+ *                             the rows are not touched
+ *   dq_weight .. dk_bias out  fp32 [D] or [H, D], written, each may be NULL; all NULL with SLA_NORM_NONE
+ * Sums over tokens in fp32 in a fixed order (no atomics): the same inputs give the same bits.
+ * Workspace: sla_qk_norm_rope_grad_workspace_bytes (may be 0 bytes: then NULL will do), 256-byte aligned.
+ */
+sla_status_t sla_qk_norm_rope_grad_workspace_bytes(const sla_heads_params_t *p, size_t *bytes);
+sla_status_t sla_qk_norm_rope_grad(const sla_heads_params_t *p, const void *q, const void *k, const float *q_weight,
+                                   const float *k_weight, const int32_t *pos, const void *dQ, const void *dK, const void *dV,
+                                   void *dq, void *dk, void *dv, float *dq_weight, float *dq_bias, float *dk_weight,
+                                   float *dk_bias, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Measurement variant of sla_forward: identical kernels and results, but every kernel is
  * bracketed by HIP events on `stream`; the call then WAITS for the stream and writes the
  * duration of each kernel in milliseconds to stage_ms[SLA_NUM_STAGES] (host memory).

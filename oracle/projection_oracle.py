@@ -1,0 +1,70 @@
+"""fp64 references of the operators around the attention: norm and rotation of heads with their gradients, the gradients of
+the FP8 layer, the microscaled 4-bit format and its linear layer.
+
+TEST INFRASTRUCTURE ONLY, numpy throughout: it never imports the GPU package and the GPU package never imports it.
+"""
+from __future__ import annotations
+
+import numpy as np
+
+from . import sla_oracle
+
+
+def bf16_to_f64(bits):
+    return (np.asarray(bits, np.uint16).astype(np.uint32) << 16).view(np.float32).astype(np.float64)
+
+
+# ---- norm and rotation of heads: rows x [B,N,H,64] of one tensor
+def _angles(pos, axes, base, pairing):
+    """(members i, members p, angle [1 or B, N, 32]) of the 32 pairs of channels; pos [N,axes] or [1 or B,N,axes]."""
+    pos = np.asarray(pos, np.float64).reshape(-1, np.shape(pos)[-2], axes)
+    S = 64 // axes
+    first, second, ang = [], [], []
+    for ax in range(axes):
+        for j in range(S // 2):
+            first.append(ax * S + (j if pairing == "halves" else 2 * j))
+            second.append(ax * S + (j + S // 2 if pairing == "halves" else 2 * j + 1))
+            ang.append(pos[..., ax] * base ** (-2.0 * j / S))
+    return first, second, np.stack(ang, -1)
+
+
+def _turn(t, axes, base, pairing, pos, back=False):
+    if axes == 0:
+        return t
+    i, p, a = _angles(pos, axes, base, pairing)
+    c, s = np.cos(a)[:, :, None, :], np.sin(a)[:, :, None, :] * (-1.0 if back else 1.0)
+    out = t.copy()
+    out[..., i] = t[..., i] * c - t[..., p] * s
+    out[..., p] = t[..., p] * c + t[..., i] * s
+    return out
+
+
+def _unit(x, norm, eps):
+    """u and r of the rows."""
+    if norm == "none":
+        return x, None
+    d = x - x.mean(-1, keepdims=True) if norm == "layer" else x
+    r = 1.0 / np.sqrt((d * d).mean(-1, keepdims=True) + eps)
+    return d * r, r
+
+
+def heads_forward(x, norm, w, b, eps, axes, pairing, base, pos):
+    """w, b: None, [64] or [H,64]."""
+    n, _ = _unit(x, norm, eps)
+    n = n if w is None else n * w
+    n = n if b is None else n + b
+    return _turn(n, axes, base, pairing, pos)
+
+
+def heads_backward(x, norm, w, eps, axes, pairing, base, pos, dy, per_head=False):
+    """(dx, dw, db); dw and db are None without a norm."""
+    d = _turn(dy, axes, base, pairing, pos, back=True)
+    u, r = _unit(x, norm, eps)
+    if r is None:
+        return d, None, None
+    over = (0, 1) if per_head else (0, 1, 2)
+    g = d if w is None else d * w
+    inner = g - (g * u).mean(-1, keepdims=True) * u
+    if norm == "layer":
+        inner = inner - g.mean(-1, keepdims=True)
+    return r * inner, (d * u).sum(over), d.sum(over)

@@ -21,6 +21,7 @@ STATE_ROWS = 65          # rows of one block state: 64 rows of h^T and one row o
 EXPORTS = ["sla_resolve_counts", "sla_workspace_bytes", "sla_forward", "sla_pool_classify", "sla_linear_states",
            "sla_marginal_aggregate", "sla_sparse_combine", "sla_forward_profiled", "sla_wproj_grad", "sla_quantise_e4m3",
            "sla_forward_with_labels", "sla_fp8_linear_workspace_bytes", "sla_fp8_linear", "sla_forward_static", "sla_sparse_combine_f32", "sla_fp8_linear_qkv",
+           "sla_qk_norm_rope", "sla_qk_norm_rope_e4m3", "sla_qk_norm_rope_grad_workspace_bytes", "sla_qk_norm_rope_grad",
            "sla_strerror", "sla_last_error", "sla_stage_name"]
 STATIC_WORKSPACE_BYTES = 96 * 1024 * 1024
 NUM_STAGES = 6
@@ -57,7 +58,7 @@ def lib() -> C.CDLL:
         _lib.sla_strerror.restype = C.c_char_p
         _lib.sla_last_error.restype = C.c_char_p
         _lib.sla_stage_name.restype = C.c_char_p
-        for name in EXPORTS[:16]:
+        for name in EXPORTS[:-3]:                    # all but the three that return text
             getattr(_lib, name).restype = C.c_int
     return _lib
 
@@ -218,3 +219,103 @@ def sla_fp8_linear_qkv(x, W, bias, B_, N, H, bq, Q8, K8, V8, sQ, sK, sV, workspa
     _check(lib().sla_fp8_linear_qkv(_ptr(x), _ptr(W), _ptr(bias), C.c_int32(B_), C.c_int32(N), C.c_int32(H), C.c_int32(d_in),
                                     C.c_int32(bq), _ptr(Q8), _ptr(K8), _ptr(V8), _ptr(sQ), _ptr(sK), _ptr(sV),
                                     _ptr(workspace), C.c_size_t(workspace.numel()), _stream()), "sla_fp8_linear_qkv")
+
+
+# ---- norm and rotation of heads
+class SlaHeadsParams(C.Structure):
+    _fields_ = [("B", C.c_int32), ("H", C.c_int32), ("N", C.c_int32), ("D", C.c_int32),
+                ("norm", C.c_int32), ("norm_per_head", C.c_int32), ("axes", C.c_int32), ("pairing", C.c_int32),
+                ("pos_per_item", C.c_int32), ("layout", C.c_int32), ("eps", C.c_float), ("base", C.c_double),
+                ("batch_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+def make_heads_params(q, norm="layer", norm_per_head=False, eps=1e-5, axes=2, pairing="halves", base=100.0, pos_per_item=False,
+                      layout="bhnd") -> SlaHeadsParams:
+    """q: a [B,N,H,64] tensor or view with the sizes and strides that q, k, v (and dq, dk, dv) have, e.g. qkv[:, :, 0] of a fused
+    projection qkv [B,N,3,H,64].  layout: of the outputs, "bhnd" or "bnhd"."""
+    Bn, N, H, D = q.shape
+    if q.stride(3) != 1 and D > 1 and q.numel():
+        raise ValueError("the 64 channels of a row must be contiguous")
+    return SlaHeadsParams(Bn, H, N, D, {"none": 0, "rms": 1, "layer": 2}[norm], int(norm_per_head), axes,
+                          {"halves": 0, "adjacent": 1}[pairing], int(pos_per_item), {"bhnd": 0, "bnhd": 1}[layout], eps, base,
+                          q.stride(0), q.stride(1), q.stride(2))
+
+
+def _tensor(t, what, dtype, shape):
+    """Pointer of a dense device tensor of this type and shape (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != shape:
+        raise ValueError(f"{what}: {dtype} {list(shape)} expected, got {t.dtype} {list(t.shape)}")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device() or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous tensor on the current device expected")
+    return t.data_ptr()
+
+
+def _rows(p, t, what):
+    """Pointer of a [B,N,H,64] tensor with the strides in p."""
+    if t is None:
+        return None
+    shape, strides = (p.B, p.N, p.H, p.D), (p.batch_stride, p.token_stride, p.head_stride, 1)
+    if t.dtype != torch.bfloat16 or tuple(t.shape) != shape or any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), strides)):
+        raise ValueError(f"{what}: bfloat16 {list(shape)} with strides {list(strides)} expected, got {t.dtype} {list(t.shape)} {list(t.stride())}")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what}: a tensor on the current device expected")
+    return t.data_ptr()
+
+
+def _heads_parameters(p, pos, *params):
+    shape = (p.H, 64) if p.norm_per_head else (64,)
+    names = ("q_weight", "q_bias", "k_weight", "k_bias")
+    ptrs = [_tensor(t, n, torch.float32, shape) for t, n in zip(params, names)]
+    full = (p.B if p.pos_per_item else 1, p.N, p.axes)
+    return ptrs, _tensor(pos, "pos", torch.int32, full[1:] if pos is not None and pos.dim() == 2 and full[0] == 1 else full)
+
+
+def _heads_shape(p):
+    return (p.B, p.N, p.H, 64) if p.layout else (p.B, p.H, p.N, 64)
+
+
+def _ptrs(ptrs):
+    return [C.c_void_p(x) for x in ptrs]
+
+
+def sla_qk_norm_rope(p, q, k, v, Q, K, V, pos=None, q_weight=None, q_bias=None, k_weight=None, k_bias=None):
+    """q, k, v bf16 [B,N,H,64] in the strides of p -> Q, K, V bf16 in p's layout; pos int32 [N,axes], [1,N,axes] or [B,N,axes]."""
+    w, at = _heads_parameters(p, pos, q_weight, q_bias, k_weight, k_bias)
+    shape = _heads_shape(p)
+    args = [_rows(p, q, "q"), _rows(p, k, "k"), _rows(p, v, "v"), *w, at, *(_tensor(t, n, torch.bfloat16, shape) for t, n in zip((Q, K, V), "QKV"))]
+    _check(lib().sla_qk_norm_rope(C.byref(p), *_ptrs(args), _stream()), "sla_qk_norm_rope")
+    return Q, K, V
+
+
+def sla_qk_norm_rope_e4m3(p, q, k, v, bq, Q8, K8, V8, sQ, sK, sV, pos=None, q_weight=None, q_bias=None, k_weight=None, k_bias=None):
+    """The same into E4M3 codes (uint8, p's layout) with block scales fp32 [B,H,ceil(N/bq)], [B,H,ceil(N/64)] twice."""
+    w, at = _heads_parameters(p, pos, q_weight, q_bias, k_weight, k_bias)
+    shape, blocks = _heads_shape(p), [(p.B, p.H, -(-p.N // max(b, 1))) for b in (bq, 64, 64)]
+    args = [_rows(p, q, "q"), _rows(p, k, "k"), _rows(p, v, "v"), *w, at]
+    out = [_tensor(t, n, torch.uint8, shape) for t, n in zip((Q8, K8, V8), ("Q8", "K8", "V8"))]
+    out += [_tensor(t, n, torch.float32, s) for t, n, s in zip((sQ, sK, sV), ("sQ", "sK", "sV"), blocks)]
+    _check(lib().sla_qk_norm_rope_e4m3(C.byref(p), *_ptrs(args), C.c_int32(bq), *_ptrs(out), _stream()), "sla_qk_norm_rope_e4m3")
+    return Q8, K8, V8, sQ, sK, sV
+
+
+def sla_qk_norm_rope_grad_workspace_bytes(p) -> int:
+    n = C.c_size_t()
+    _check(lib().sla_qk_norm_rope_grad_workspace_bytes(C.byref(p), C.byref(n)), "sla_qk_norm_rope_grad_workspace_bytes")
+    return n.value
+
+
+def sla_qk_norm_rope_grad(p, q, k, dQ, dK, dV, dq, dk, dv, pos=None, q_weight=None, k_weight=None, dq_weight=None, dq_bias=None,
+                          dk_weight=None, dk_bias=None, workspace=None):
+    """dQ, dK, dV (bf16, p's layout) -> dq, dk, dv (bf16, the strides of q, k, v) and fp32 gradients of the norm's parameters."""
+    w, at = _heads_parameters(p, pos, q_weight, None, k_weight, None)
+    dw, _ = _heads_parameters(p, None, dq_weight, dq_bias, dk_weight, dk_bias)
+    shape = _heads_shape(p)
+    if workspace is None:
+        workspace = torch.empty(max(256, sla_qk_norm_rope_grad_workspace_bytes(p)), dtype=torch.uint8, device=q.device)
+    args = [_rows(p, q, "q"), _rows(p, k, "k"), w[0], w[2], at, *(_tensor(t, n, torch.bfloat16, shape) for t, n in zip((dQ, dK, dV), ("dQ", "dK", "dV"))),
+            _rows(p, dq, "dq"), _rows(p, dk, "dk"), _rows(p, dv, "dv"), *dw]
+    _check(lib().sla_qk_norm_rope_grad(C.byref(p), *_ptrs(args), _ptr(workspace), C.c_size_t(workspace.numel()), _stream()),
+           "sla_qk_norm_rope_grad")
+    return dq, dk, dv

@@ -1,7 +1,6 @@
 // C ABI of the SLA forward: parameter validation, workspace carving and kernel sequencing.
 // Host code only; every device operation is a kernel launch on the caller's stream.
-#include "../../include/sla.h"
-#include "sla_common.hpp"
+#include "api_util.hpp"
 #include "sla_kernels.hpp"
 
 #include <cmath>
@@ -14,9 +13,8 @@
 // the code object is loaded until the process ends.  In host code the name is only a handle for hipGetSymbolAddress.
 static __device__ __align__(256) unsigned char g_static_workspace[SLA_STATIC_WORKSPACE_BYTES];
 
-namespace {
-
-thread_local char g_err[512] = "";
+namespace sla {
+static thread_local char g_err[512] = "";
 
 sla_status_t fail(sla_status_t st, const char *fmt, ...)
 {
@@ -26,9 +24,14 @@ sla_status_t fail(sla_status_t st, const char *fmt, ...)
     va_end(ap);
     return st;
 }
+}  // namespace sla
 
-size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
+using sla::aligned;
+using sla::align_up;
+using sla::at;
+using sla::fail;
+
+namespace {
 
 struct Plan {
     int BH, Nqb, Nkb, k_c, k_n, lab_pitch, s_pitch, nW;
@@ -110,23 +113,6 @@ sla_status_t check_ws(const Plan &pl, const void *ws, size_t bytes)
     return SLA_OK;
 }
 
-#define SLA_REQ_PTR(ptr)                                                                              \
-    do {                                                                                              \
-        if (!(ptr)) return fail(SLA_ERR_INVALID_ARG, #ptr " is NULL");                                \
-        if (!aligned((ptr), 16)) return fail(SLA_ERR_INVALID_ARG, #ptr " must be 16-byte aligned");   \
-    } while (0)
-#define SLA_OPT_PTR(ptr)                                                                              \
-    do {                                                                                              \
-        if ((ptr) && !aligned((ptr), 16)) return fail(SLA_ERR_INVALID_ARG, #ptr " must be 16-byte aligned"); \
-    } while (0)
-#define SLA_HIP(call)                                                                                 \
-    do {                                                                                              \
-        hipError_t e_ = (call);                                                                       \
-        if (e_ != hipSuccess) return fail(SLA_ERR_HIP, "%s failed: %s", #call, hipGetErrorString(e_)); \
-    } while (0)
-
-template <class T> T *at(void *ws, size_t off) { return (T *)((char *)ws + off); }
-
 // Pooling, pooled logits and classifier.  Leaves the marginal bit masks and the critical lists in the workspace.
 sla_status_t run_classify(const sla_params_t *p, const Plan &pl, const void *Q, const void *K, const float *sQ,
                           const float *sK, int8_t *labels, int32_t *crit_out, float *Pc, double *qbar_out,
@@ -181,7 +167,7 @@ const char *sla_strerror(sla_status_t s)
     return "unknown status";
 }
 
-const char *sla_last_error(void) { return g_err; }
+const char *sla_last_error(void) { return sla::g_err; }
 
 sla_status_t sla_resolve_counts(const sla_params_t *p, int32_t *k_crit, int32_t *k_neg)
 {

@@ -92,4 +92,31 @@ int fp8_gemm_qkv_token_tile(int M, int H);
 hipError_t launch_fp8_gemm_qkv(const void *A8, const float *sa, const void *W8, const float *sw, const void *bias, int B, int N, int H, int K,
                                int bq, void *const codes[3], float *const scales[3], hipStream_t st);
 
+// Norm and rotation of the heads of a projection's output (k_heads.hip).  Strides in elements; x and y [0..2] = q, k, v.
+struct HeadsArgs {
+    const uint16_t *x[3];       // inputs, row (b, t, h) at b bs + t ts + h hs
+    void *y[3];                 // outputs, row at b obs + t ots + h ohs: bf16, or E4M3 codes with
+    float *scales[3];           // their block scales [B,H,blocks]
+    const float *w[2], *b[2];   // weights and biases of the norm, [64] or [H,64]; NULL = 1 and 0
+    const int32_t *pos;         // positions [N or B N, axes]
+    long bs, ts, hs, obs, ots, ohs;
+    int B, H, N, tensors;       // tensors: 2 (no v) or 3
+    int norm, per_head, axes, adjacent, pos_per_item;     // norm: 0 none, 1 RMS, 2 layer
+    float eps;
+    int chunk, splits;          // set by the launch: (tensor, head) items of a workgroup, workgroups of a token block
+    double turn[32];            // turns per unit of position, of every angle of the table (k_heads.hip)
+};
+struct HeadsGrads {
+    const uint16_t *g[3];       // gradients of y
+    uint16_t *dx[3];            // gradients of x
+    float *dw[2], *db[2];       // [64] or [H,64], each may be NULL
+    float *part;                // scratch of heads_grad_part_bytes bytes, NULL if none of them is wanted
+    int slots;                  // set by the launch
+};
+// bq: 0 = bf16 outputs; 64, 128 = E4M3 with query blocks of bq tokens (64 for k and v)
+hipError_t launch_heads(const HeadsArgs &a, int bq, hipStream_t st);
+size_t heads_grad_part_bytes(int B, int H, int N, int tensors, int per_head);
+// with B N = 0 the gradients of the weights are set to zero
+hipError_t launch_heads_grad(const HeadsArgs &a, const HeadsGrads &d, hipStream_t st);
+
 }  // namespace sla
