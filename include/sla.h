@@ -203,6 +203,29 @@ sla_status_t sla_fp8_linear_qkv(const void *x, const void *W, const void *bias, 
                                 void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Training of that layer (Alg. 2; straight through both quantisers) with its input kept in 8 bits.  sla_fp8_linear_save is
+ * sla_fp8_linear (the same y, bit for bit) that leaves the E4M3 codes and the scales of x, which it multiplies anyway, in
+ * `checkpoint`: sla_fp8_checkpoint_bytes(N, d_in), about N (d_in + 4) bytes, half of x; x itself is not needed again.
+ * sla_fp8_linear_grad takes them for the gradients
+ *     dx = dy W_q     dW = dy^T x_q     db = sum over tokens of dy        x_q, W_q = bf16(code * scale)
+ * with products summed in fp32 in a fixed order (no atomics: the same inputs give the same bits) and rounded once to bf16.
+ *   x, W, bias, y   as sla_fp8_linear; W in sla_fp8_linear_grad is that of the forward (quantised again; needed for dx only)
+ *   dy    in   bf16 [N, d_out]
+ *   dx    out  bf16 [N, d_in] or NULL;   dW  out  bf16 [d_out, d_in] or NULL;   db  out  bf16 [d_out] or NULL (only with dW)
+ *   workspace  sla_fp8_linear_grad_workspace_bytes(N, d_in, d_out) bytes for both calls, 256-byte aligned as the checkpoint;
+ *              it holds nothing from one call to the next
+ * With N = 0, dW and db are set to zero (workspace, checkpoint and dy may be NULL).
+ * sla_fp8_checkpoint_restore writes x_q [N, d_in], bf16, for what else of a backward pass needs the layer's input.
+ */
+sla_status_t sla_fp8_checkpoint_bytes(int32_t N, int32_t d_in, size_t *bytes);
+sla_status_t sla_fp8_checkpoint_restore(const void *checkpoint, size_t checkpoint_bytes, int32_t N, int32_t d_in, void *x, void *stream);
+sla_status_t sla_fp8_linear_grad_workspace_bytes(int32_t N, int32_t d_in, int32_t d_out, size_t *bytes);
+sla_status_t sla_fp8_linear_save(const void *x, const void *W, const void *bias, int32_t N, int32_t d_in, int32_t d_out, void *y,
+                                 void *checkpoint, size_t checkpoint_bytes, void *workspace, size_t workspace_bytes, void *stream);
+sla_status_t sla_fp8_linear_grad(const void *dy, const void *checkpoint, size_t checkpoint_bytes, const void *W, int32_t N, int32_t d_in,
+                                 int32_t d_out, void *dx, void *dW, void *db, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Norm of every head's queries and keys and position rotation, in one pass from a projection's output to the form the
  * attention takes its inputs in.  For every token and head, over the 64 channels of its row x of q (and of k):
  *     u = (x - m) r,  r = 1 / sqrt(mean((x - m)^2) + eps)      m = mean(x) (SLA_NORM_LAYER), 0 (SLA_NORM_RMS)

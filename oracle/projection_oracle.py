@@ -68,3 +68,17 @@ def heads_backward(x, norm, w, eps, axes, pairing, base, pos, dy, per_head=False
     if norm == "layer":
         inner = inner - g.mean(-1, keepdims=True)
     return r * inner, (d * u).sum(over), d.sum(over)
+
+
+# ---- the FP8 layer's gradients
+def e4m3_rows(bits):
+    """(values, scales) of bf16 rows as the layer quantises them: E4M3 numbers, one fp32 scale per row."""
+    codes, scales = sla_oracle.quantise_e4m3_rows(bits)
+    grid = sla_oracle._e4m3_grid()
+    return np.where(codes & 0x80, -1.0, 1.0) * grid[(codes & 0x7F).astype(np.int64)], scales.astype(np.float64)
+
+
+def fp8_linear_backward(x_bits, W_bits, dy):
+    """(dx, dW, db), straight through both quantisers; dy float64 [N, d_out]."""
+    (xc, xs), (wc, ws) = e4m3_rows(x_bits), e4m3_rows(W_bits)
+    return dy @ (wc * ws[:, None]), dy.T @ (xc * xs[:, None]), dy.sum(0)

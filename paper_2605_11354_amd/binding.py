@@ -21,6 +21,7 @@ STATE_ROWS = 65          # rows of one block state: 64 rows of h^T and one row o
 EXPORTS = ["sla_resolve_counts", "sla_workspace_bytes", "sla_forward", "sla_pool_classify", "sla_linear_states",
            "sla_marginal_aggregate", "sla_sparse_combine", "sla_forward_profiled", "sla_wproj_grad", "sla_quantise_e4m3",
            "sla_forward_with_labels", "sla_fp8_linear_workspace_bytes", "sla_fp8_linear", "sla_forward_static", "sla_sparse_combine_f32", "sla_fp8_linear_qkv",
+           "sla_fp8_checkpoint_bytes", "sla_fp8_checkpoint_restore", "sla_fp8_linear_grad_workspace_bytes", "sla_fp8_linear_save", "sla_fp8_linear_grad",
            "sla_qk_norm_rope", "sla_qk_norm_rope_e4m3", "sla_qk_norm_rope_grad_workspace_bytes", "sla_qk_norm_rope_grad",
            "sla_strerror", "sla_last_error", "sla_stage_name"]
 STATIC_WORKSPACE_BYTES = 96 * 1024 * 1024
@@ -319,3 +320,58 @@ def sla_qk_norm_rope_grad(p, q, k, dQ, dK, dV, dq, dk, dv, pos=None, q_weight=No
     _check(lib().sla_qk_norm_rope_grad(C.byref(p), *_ptrs(args), _ptr(workspace), C.c_size_t(workspace.numel()), _stream()),
            "sla_qk_norm_rope_grad")
     return dq, dk, dv
+
+
+# ---- training of the FP8 layer from an 8-bit copy of its input
+def _bytes(name, *sizes) -> int:
+    n = C.c_size_t()
+    _check(getattr(lib(), name)(*[C.c_int32(x) for x in sizes], C.byref(n)), name)
+    return n.value
+
+
+def sla_fp8_checkpoint_bytes(N, d_in) -> int:
+    return _bytes("sla_fp8_checkpoint_bytes", N, d_in)
+
+
+def sla_fp8_linear_grad_workspace_bytes(N, d_in, d_out) -> int:
+    return _bytes("sla_fp8_linear_grad_workspace_bytes", N, d_in, d_out)
+
+
+def _buffer(t, what):
+    """(pointer, bytes) of a checkpoint or workspace."""
+    p = _tensor(t, what, torch.uint8, (t.numel(),))
+    return C.c_void_p(p), C.c_size_t(t.numel())
+
+
+def _linear_workspace(workspace, N, d_in, d_out, device):
+    if workspace is None:
+        workspace = torch.empty(max(256, sla_fp8_linear_grad_workspace_bytes(N, d_in, d_out)), dtype=torch.uint8, device=device)
+    return _buffer(workspace, "workspace")
+
+
+def sla_fp8_linear_save(x, W, bias, y, checkpoint, workspace=None):
+    """sla_fp8_linear that leaves x in 8 bits in `checkpoint` (uint8, sla_fp8_checkpoint_bytes(N, d_in) long)."""
+    (N, d_in), d_out, bf = x.shape, W.shape[0], torch.bfloat16
+    args = _ptrs([_tensor(x, "x", bf, (N, d_in)), _tensor(W, "W", bf, (d_out, d_in)), _tensor(bias, "bias", bf, (d_out,))])
+    _check(lib().sla_fp8_linear_save(*args, C.c_int32(N), C.c_int32(d_in), C.c_int32(d_out), C.c_void_p(_tensor(y, "y", bf, (N, d_out))),
+                                     *_buffer(checkpoint, "checkpoint"), *_linear_workspace(workspace, N, d_in, d_out, x.device), _stream()),
+           "sla_fp8_linear_save")
+    return y
+
+
+def sla_fp8_linear_grad(dy, checkpoint, W, dx=None, dW=None, db=None, workspace=None):
+    """Gradients of sla_fp8_linear_save's x, W and bias (each may be None; db only with dW) from that of its y."""
+    (N, d_out), d_in, bf = dy.shape, W.shape[1], torch.bfloat16
+    out = _ptrs([_tensor(dx, "dx", bf, (N, d_in)), _tensor(dW, "dW", bf, (d_out, d_in)), _tensor(db, "db", bf, (d_out,))])
+    _check(lib().sla_fp8_linear_grad(C.c_void_p(_tensor(dy, "dy", bf, (N, d_out))), *_buffer(checkpoint, "checkpoint"),
+                                     C.c_void_p(_tensor(W, "W", bf, (d_out, d_in))), C.c_int32(N), C.c_int32(d_in), C.c_int32(d_out), *out,
+                                     *_linear_workspace(workspace, N, d_in, d_out, dy.device), _stream()), "sla_fp8_linear_grad")
+    return dx, dW, db
+
+
+def sla_fp8_checkpoint_restore(checkpoint, x):
+    """x bf16 [N,d_in] <- the layer's input as its forward multiplied it."""
+    N, d_in = x.shape
+    _check(lib().sla_fp8_checkpoint_restore(*_buffer(checkpoint, "checkpoint"), C.c_int32(N), C.c_int32(d_in),
+                                            C.c_void_p(_tensor(x, "x", torch.bfloat16, (N, d_in))), _stream()), "sla_fp8_checkpoint_restore")
+    return x

@@ -486,6 +486,118 @@ sla_status_t sla_fp8_linear_qkv(const void *x, const void *W, const void *bias, 
     return SLA_OK;
 }
 
+namespace {
+// The 8-bit copy of a layer's input: codes in fragment order, then one scale per token.
+struct CheckpointPlan { size_t off_scales, total; };
+sla_status_t make_checkpoint_plan(int32_t N, int32_t d_in, CheckpointPlan &cp)
+{
+    LinPlan lp;
+    sla_status_t s = make_lin_plan(N, d_in, 8, lp);
+    if (s != SLA_OK) return s;
+    cp.off_scales = align_up((size_t)N * d_in, 256);
+    cp.total = cp.off_scales + align_up((size_t)N * sizeof(float), 256);
+    return SLA_OK;
+}
+sla_status_t check_buffer(const char *name, const void *buf, size_t bytes, size_t need)
+{
+    if (!buf) return fail(SLA_ERR_WORKSPACE, "%s is NULL (%zu bytes needed)", name, need);
+    if (!aligned(buf, 256)) return fail(SLA_ERR_WORKSPACE, "%s must be 256-byte aligned", name);
+    if (bytes < need) return fail(SLA_ERR_WORKSPACE, "%s has %zu bytes, %zu needed", name, bytes, need);
+    return SLA_OK;
+}
+// Workspace of the layer's training calls: codes and scales of W, partial sums of dW and db.
+struct LinGradPlan { size_t off_sw, off_part, total; };
+sla_status_t make_lin_grad_plan(int32_t N, int32_t d_in, int32_t d_out, LinGradPlan &gp)
+{
+    LinPlan lp;
+    sla_status_t s = make_lin_plan(N, d_in, d_out, lp);
+    if (s != SLA_OK) return s;
+    if ((double)N * d_out >= 4.0e9) return fail(SLA_ERR_UNSUPPORTED, "gradient of 4e9 values or more");
+    gp.off_sw = align_up((size_t)d_out * d_in, 256);
+    gp.off_part = gp.off_sw + align_up((size_t)d_out * sizeof(float), 256);
+    gp.total = gp.off_part + align_up((size_t)sla::linear_grad_splits(N, d_in, d_out) * d_out * ((size_t)d_in + 1) * sizeof(float), 256);
+    return SLA_OK;
+}
+}  // namespace
+
+sla_status_t sla_fp8_checkpoint_bytes(int32_t N, int32_t d_in, size_t *bytes)
+{
+    CheckpointPlan cp;
+    sla_status_t s = make_checkpoint_plan(N, d_in, cp);
+    if (s != SLA_OK) return s;
+    if (!bytes) return fail(SLA_ERR_INVALID_ARG, "bytes is NULL");
+    *bytes = cp.total;
+    return SLA_OK;
+}
+
+sla_status_t sla_fp8_checkpoint_restore(const void *checkpoint, size_t checkpoint_bytes, int32_t N, int32_t d_in, void *x, void *stream)
+{
+    CheckpointPlan cp;
+    sla_status_t s = make_checkpoint_plan(N, d_in, cp);
+    if (s != SLA_OK) return s;
+    if (N == 0) return SLA_OK;
+    SLA_REQ_PTR(x);
+    if ((s = check_buffer("checkpoint", checkpoint, checkpoint_bytes, cp.total)) != SLA_OK) return s;
+    SLA_HIP(sla::launch_restore_rows(checkpoint, (const float *)((const char *)checkpoint + cp.off_scales), N, d_in, x, (hipStream_t)stream));
+    return SLA_OK;
+}
+
+sla_status_t sla_fp8_linear_grad_workspace_bytes(int32_t N, int32_t d_in, int32_t d_out, size_t *bytes)
+{
+    LinGradPlan gp;
+    sla_status_t s = make_lin_grad_plan(N, d_in, d_out, gp);
+    if (s != SLA_OK) return s;
+    if (!bytes) return fail(SLA_ERR_INVALID_ARG, "bytes is NULL");
+    *bytes = gp.total;
+    return SLA_OK;
+}
+
+sla_status_t sla_fp8_linear_save(const void *x, const void *W, const void *bias, int32_t N, int32_t d_in, int32_t d_out, void *y,
+                                 void *checkpoint, size_t checkpoint_bytes, void *workspace, size_t workspace_bytes, void *stream)
+{
+    CheckpointPlan cp;
+    LinGradPlan gp;
+    sla_status_t s = make_lin_grad_plan(N, d_in, d_out, gp);
+    if (s != SLA_OK || (s = make_checkpoint_plan(N, d_in, cp)) != SLA_OK) return s;
+    if (N == 0) return SLA_OK;
+    SLA_REQ_PTR(x); SLA_REQ_PTR(W); SLA_REQ_PTR(y);
+    SLA_OPT_PTR(bias);
+    if ((s = check_buffer("checkpoint", checkpoint, checkpoint_bytes, cp.total)) != SLA_OK) return s;
+    if ((s = check_buffer("workspace", workspace, workspace_bytes, gp.total)) != SLA_OK) return s;
+    hipStream_t st = (hipStream_t)stream;
+    float *const sx = at<float>(checkpoint, cp.off_scales), *const sw = at<float>(workspace, gp.off_sw);
+    SLA_HIP(sla::launch_quantise_rows(x, N, checkpoint, sx, W, d_out, workspace, sw, d_in, st));
+    SLA_HIP(sla::launch_fp8_gemm(checkpoint, sx, workspace, sw, bias, N, d_out, d_in, y, st));
+    return SLA_OK;
+}
+
+sla_status_t sla_fp8_linear_grad(const void *dy, const void *checkpoint, size_t checkpoint_bytes, const void *W, int32_t N, int32_t d_in,
+                                 int32_t d_out, void *dx, void *dW, void *db, void *workspace, size_t workspace_bytes, void *stream)
+{
+    CheckpointPlan cp;
+    LinGradPlan gp;
+    sla_status_t s = make_lin_grad_plan(N, d_in, d_out, gp);
+    if (s != SLA_OK || (s = make_checkpoint_plan(N, d_in, cp)) != SLA_OK) return s;
+    SLA_OPT_PTR(dx); SLA_OPT_PTR(dW); SLA_OPT_PTR(db);
+    if (db && !dW) return fail(SLA_ERR_UNSUPPORTED, "db comes with dW");
+    if (N > 0 && (dx || dW)) {
+        SLA_REQ_PTR(dy);
+        if (dx) SLA_REQ_PTR(W);
+        if (dW && (s = check_buffer("checkpoint", checkpoint, checkpoint_bytes, cp.total)) != SLA_OK) return s;
+        if ((s = check_buffer("workspace", workspace, workspace_bytes, gp.total)) != SLA_OK) return s;
+    }
+    hipStream_t st = (hipStream_t)stream;
+    if (dx && N > 0) {
+        float *const sw = at<float>(workspace, gp.off_sw);
+        SLA_HIP(sla::launch_quantise_rows(nullptr, 0, nullptr, nullptr, W, d_out, workspace, sw, d_in, st));
+        SLA_HIP(sla::launch_linear_dx(dy, workspace, sw, N, d_in, d_out, dx, st));
+    }
+    if (dW)
+        SLA_HIP(sla::launch_linear_dw(dy, checkpoint, (const float *)((const char *)checkpoint + cp.off_scales), N, d_in, d_out, dW, db,
+                                      at<float>(workspace, gp.off_part), st));
+    return SLA_OK;
+}
+
 const char *sla_stage_name(int stage)
 {
     static const char *names[SLA_NUM_STAGES] = {"pool_q", "states", "scores", "select", "aggregate", "attend"};
