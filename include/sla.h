@@ -226,6 +226,32 @@ sla_status_t sla_fp8_linear_grad(const void *dy, const void *checkpoint, size_t 
                                  int32_t d_out, void *dx, void *dW, void *db, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Microscaled 4-bit floating point (the OCP MX format with E2M1 elements): every 32 consecutive elements of a row are E2M1
+ * numbers (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives: codes 0 .. 7 and 8 .. 15) times a power of two 2^(s - 127).
+ *   codes   uint8 [rows, cols/2], the even element in the low half of a byte;   scales  uint8 [rows, cols/32], the s
+ * sla_quantise_mxfp4: s = max(floor(log2(amax)) + 125, 0) of the block's largest magnitude (0 for a block of zeros), codes to
+ * nearest even, magnitudes above 6 become 6; a block with an infinity or NaN gets s = 255 and codes 0.  Defined bit for bit.
+ * sla_dequantise_mxfp4: the numbers as bf16 (exact while they are finite in bf16); s = 255 gives NaN.
+ *   X, Y  bf16 [rows, cols], cols a multiple of 32
+ */
+sla_status_t sla_quantise_mxfp4(const void *X, int64_t rows, int32_t cols, void *codes, void *scales, void *stream);
+sla_status_t sla_dequantise_mxfp4(const void *codes, const void *scales, int64_t rows, int32_t cols, void *Y, void *stream);
+
+/*
+ * Linear layer with weights in that form, for serving: x is quantised as sla_quantise_mxfp4 does, then y = x4 W4^T + bias with
+ * exact products, fp32 sums and one rounding to bf16.  At most 32 tokens (a decoding step) take one launch and no workspace.
+ *   x      in   bf16 [N, d_in]                      d_in a multiple of 128
+ *   W      in   codes uint8 [d_out, d_in/2] and scales uint8 [d_out, d_in/32]      d_out a multiple of 8
+ *   bias   in   bf16 [d_out] or NULL
+ *   y      out  bf16 [N, d_out]
+ *   workspace  sla_mxfp4_linear_workspace_bytes(N, d_in, d_out) bytes (may be 0: then NULL will do), 256-byte aligned
+ * A token with an infinity or NaN, or one that meets a weight block with s = 255, comes out NaN; others are not affected.
+ */
+sla_status_t sla_mxfp4_linear_workspace_bytes(int32_t N, int32_t d_in, int32_t d_out, size_t *bytes);
+sla_status_t sla_mxfp4_linear(const void *x, const void *W_codes, const void *W_scales, const void *bias, int32_t N, int32_t d_in,
+                              int32_t d_out, void *y, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Norm of every head's queries and keys and position rotation, in one pass from a projection's output to the form the
  * attention takes its inputs in.  For every token and head, over the 64 channels of its row x of q (and of k):
  *     u = (x - m) r,  r = 1 / sqrt(mean((x - m)^2) + eps)      m = mean(x) (SLA_NORM_LAYER), 0 (SLA_NORM_RMS)

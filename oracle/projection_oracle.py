@@ -82,3 +82,33 @@ def fp8_linear_backward(x_bits, W_bits, dy):
     """(dx, dW, db), straight through both quantisers; dy float64 [N, d_out]."""
     (xc, xs), (wc, ws) = e4m3_rows(x_bits), e4m3_rows(W_bits)
     return dy @ (wc * ws[:, None]), dy.T @ (xc * xs[:, None]), dy.sum(0)
+
+
+# ---- microscaled 4-bit numbers: by search through the sixteen numbers, ties to the even code
+E2M1 = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def mxfp4_quantise(bits):
+    """(codes [rows, cols] 0 .. 15, scales [rows, cols/32]) of bf16 bit patterns [rows, cols]."""
+    bits = np.asarray(bits, np.uint16)
+    x = bf16_to_f64(bits).reshape(bits.shape[0], -1, 32)
+    bad = ~np.isfinite(x).all(-1)
+    mag = np.where(bad[..., None], 0.0, np.abs(x))
+    s = np.maximum(np.where(mag.max(-1) > 0, np.frexp(mag.max(-1))[1] - 1, -200) + 125, 0)
+    v = mag * np.ldexp(1.0, 127 - s)[..., None]
+    d = np.abs(np.minimum(v, 6.0)[..., None] - E2M1)
+    best = d.min(-1, keepdims=True)
+    code = np.where(d == best, np.arange(8) + 8 * (np.arange(8) % 2), 99).min(-1) % 8        # of two at the same distance the even one
+    code = code + 8 * (bits.reshape(x.shape) >> 15)
+    code[bad] = 0
+    return code.reshape(bits.shape), np.where(bad, 255, s)
+
+
+def mxfp4_values(codes, scales):
+    v = np.where(codes & 8, -1.0, 1.0) * E2M1[codes & 7]
+    p = np.where(scales == 255, np.nan, np.ldexp(1.0, np.where(scales == 255, 0, scales) - 127))
+    return v * np.repeat(p, 32, 1)
+
+
+def mxfp4_pack(codes):
+    return (codes[:, 0::2] | codes[:, 1::2] << 4).astype(np.uint8)

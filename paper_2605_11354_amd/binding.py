@@ -22,6 +22,7 @@ EXPORTS = ["sla_resolve_counts", "sla_workspace_bytes", "sla_forward", "sla_pool
            "sla_marginal_aggregate", "sla_sparse_combine", "sla_forward_profiled", "sla_wproj_grad", "sla_quantise_e4m3",
            "sla_forward_with_labels", "sla_fp8_linear_workspace_bytes", "sla_fp8_linear", "sla_forward_static", "sla_sparse_combine_f32", "sla_fp8_linear_qkv",
            "sla_fp8_checkpoint_bytes", "sla_fp8_checkpoint_restore", "sla_fp8_linear_grad_workspace_bytes", "sla_fp8_linear_save", "sla_fp8_linear_grad",
+           "sla_quantise_mxfp4", "sla_dequantise_mxfp4", "sla_mxfp4_linear_workspace_bytes", "sla_mxfp4_linear",
            "sla_qk_norm_rope", "sla_qk_norm_rope_e4m3", "sla_qk_norm_rope_grad_workspace_bytes", "sla_qk_norm_rope_grad",
            "sla_strerror", "sla_last_error", "sla_stage_name"]
 STATIC_WORKSPACE_BYTES = 96 * 1024 * 1024
@@ -375,3 +376,38 @@ def sla_fp8_checkpoint_restore(checkpoint, x):
     _check(lib().sla_fp8_checkpoint_restore(*_buffer(checkpoint, "checkpoint"), C.c_int32(N), C.c_int32(d_in),
                                             C.c_void_p(_tensor(x, "x", torch.bfloat16, (N, d_in))), _stream()), "sla_fp8_checkpoint_restore")
     return x
+
+
+# ---- microscaled 4-bit numbers
+def sla_quantise_mxfp4(X, codes, scales):
+    """X bf16 [rows, cols] -> codes uint8 [rows, cols/2], scales uint8 [rows, cols/32]."""
+    rows, cols = X.shape
+    args = _ptrs([_tensor(codes, "codes", torch.uint8, (rows, cols // 2)), _tensor(scales, "scales", torch.uint8, (rows, cols // 32))])
+    _check(lib().sla_quantise_mxfp4(C.c_void_p(_tensor(X, "X", torch.bfloat16, (rows, cols))), C.c_int64(rows), C.c_int32(cols), *args, _stream()),
+           "sla_quantise_mxfp4")
+    return codes, scales
+
+
+def sla_dequantise_mxfp4(codes, scales, Y):
+    """Y bf16 [rows, cols] <- the numbers that codes and scales stand for."""
+    rows, cols = Y.shape
+    args = _ptrs([_tensor(codes, "codes", torch.uint8, (rows, cols // 2)), _tensor(scales, "scales", torch.uint8, (rows, cols // 32))])
+    _check(lib().sla_dequantise_mxfp4(*args, C.c_int64(rows), C.c_int32(cols), C.c_void_p(_tensor(Y, "Y", torch.bfloat16, (rows, cols))), _stream()),
+           "sla_dequantise_mxfp4")
+    return Y
+
+
+def sla_mxfp4_linear_workspace_bytes(N, d_in, d_out) -> int:
+    return _bytes("sla_mxfp4_linear_workspace_bytes", N, d_in, d_out)
+
+
+def sla_mxfp4_linear(x, W_codes, W_scales, bias, y, workspace=None):
+    """y bf16 [N,d_out] <- linear layer of x bf16 [N,d_in], both factors in microscaled 4-bit numbers."""
+    (N, d_in), d_out, bf = x.shape, W_codes.shape[0], torch.bfloat16
+    args = _ptrs([_tensor(x, "x", bf, (N, d_in)), _tensor(W_codes, "W_codes", torch.uint8, (d_out, d_in // 2)),
+                  _tensor(W_scales, "W_scales", torch.uint8, (d_out, d_in // 32)), _tensor(bias, "bias", bf, (d_out,))])
+    if workspace is None:
+        workspace = torch.empty(max(256, sla_mxfp4_linear_workspace_bytes(N, d_in, d_out)), dtype=torch.uint8, device=x.device)
+    _check(lib().sla_mxfp4_linear(*args, C.c_int32(N), C.c_int32(d_in), C.c_int32(d_out), C.c_void_p(_tensor(y, "y", bf, (N, d_out))),
+                                  *_buffer(workspace, "workspace"), _stream()), "sla_mxfp4_linear")
+    return y

@@ -1,0 +1,302 @@
+// Microscaled 4-bit floating point: 32 consecutive elements of a row share a power of two 2^(s - 127), s one byte, and are
+// E2M1 numbers c (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), two to a byte, the even element in the low half.
+//     s = max(exponent field of the block's largest magnitude - 2, 0),   c = E2M1(x 2^(127 - s)), to nearest even, at most 6
+// A block with an infinity or NaN gets s = 255 (NaN) and codes 0.  The linear layer
+//     y[i][o] = sum over blocks of 2^(sx + sw - 254) sum of c_x c_w + bias[o]
+// runs on the scaled matrix instructions, which take both scales beside the codes: products are exact, sums are fp32.
+#include "sla_common.hpp"
+#include "sla_kernels.hpp"
+
+#include <type_traits>
+
+namespace sla {
+
+namespace {
+constexpr int kFp4 = 4;                              // operand format of the scaled matrix instructions
+
+// largest magnitude of eight bf16 (bits without the sign; infinities and NaN order above all numbers)
+__device__ __forceinline__ uint32_t top_bits(uint4 u)
+{
+    typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+    auto mag = [](uint32_t w) { return __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu); };
+    const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(mag(u.x), mag(u.y)), __builtin_elementwise_max(mag(u.z), mag(u.w)));
+    return m[0] > m[1] ? m[0] : m[1];
+}
+// scale byte of a block with that largest magnitude
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top) { return top >= 0x7F80u ? 255u : (top >> 7) < 2 ? 0u : (top >> 7) - 2; }
+
+// eight codes of eight bf16; scale = 2^(s - 127) as fp32 bits (subnormal for s = 0).  Blocks with s = 255 are the caller's.
+__device__ __forceinline__ uint32_t codes8(uint4 u, float scale)
+{
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, u.x), scale, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, u.y), scale, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, u.z), scale, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, u.w), scale, 3);
+}
+__device__ __forceinline__ float scale_value(uint32_t s) { return __uint_as_float(s ? s << 23 : 0x00400000u); }
+}  // namespace
+
+// Four lanes to a block, 16 bytes of it each: 2 bytes in, 17/32 out per element, bound by HBM.
+__global__ __launch_bounds__(256) void quantise_mxfp4_kernel(const uint4 *__restrict__ X, long pieces, uint32_t *__restrict__ codes, uint8_t *__restrict__ scales)
+{
+    const long at = (long)blockIdx.x * 256 + threadIdx.x;      // pieces is a multiple of four: a block's lanes all work or all leave
+    if (at >= pieces) return;
+    const uint4 u = X[at];
+    uint32_t top = top_bits(u);
+    top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0xB1, 0xf, 0xf, true));
+    top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0x4E, 0xf, 0xf, true));
+    const uint32_t s = scale_byte(top);
+    codes[at] = s == 255 ? 0u : codes8(u, scale_value(s));
+    if ((at & 3) == 0) scales[at >> 2] = (uint8_t)s;
+}
+
+// Eight elements a thread.
+__global__ __launch_bounds__(256) void dequantise_mxfp4_kernel(const uint32_t *__restrict__ codes, const uint8_t *__restrict__ scales, long pieces, uint4 *__restrict__ Y)
+{
+    const long at = (long)blockIdx.x * 256 + threadIdx.x;
+    if (at >= pieces) return;
+    const uint32_t c = codes[at], s = scales[at >> 2];
+    const float scale = s == 255 ? __builtin_nanf("") : scale_value(s);
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t m = (c >> (4 * e)) & 7;       // 2 |c|: 0 1 2 3 4 6 8 12, sixteen to a dword pair
+        const float mag = 0.5f * (float)((0xC8643210u >> (4 * m)) & 15u);
+        v[e] = ((c >> (4 * e)) & 8 ? -mag : mag) * scale;
+    }
+    Y[at] = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+}
+
+// Large products.  A [M, K] tokens, W [O, K] channels: codes (K / 2 bytes a row) and scales (K / 32 bytes a row) as they lie.
+// Workgroup tile 64 TB tokens x 128 channels, four waves as 2 x 2; steps of 128 elements: 64 bytes and one dword of
+// scales of every row.  In LDS the 16-byte piece c of row r is at position c ^ (r / 4 % 4): sixteen rows' reads of one piece
+// meet all banks once.  D[o][i] (W is the first operand): a lane's four consecutive registers are consecutive channels.
+template <int TB>
+__global__ __launch_bounds__(256, 2) void mxfp4_gemm_kernel(const uint8_t *__restrict__ A, const uint8_t *__restrict__ As, const uint8_t *__restrict__ W,
+                                                            const uint8_t *__restrict__ Ws, const uint16_t *__restrict__ bias, int M, int O, int K,
+                                                            int n_ot, int total, uint16_t *__restrict__ Y)
+{
+    constexpr int kTok = 64 * TB, kRows = kTok + 128, kStage = kRows * 68;       // codes of all rows, then their scales
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * kStage];
+    const int item = (int)xcd_remap(blockIdx.x, total);
+    if (item >= total) return;
+    const int it = (int)((unsigned)item / (unsigned)n_ot), ot = item - it * n_ot;
+    const int i0 = it * kTok, o0 = ot * 128;
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wo = (wave >> 1) * 64, wi = (wave & 1) * (32 * TB);
+
+    // what a thread brings in: TB pieces of tokens' rows and two of channels' rows (row id / 4, piece id % 4), one dword of
+    // scales of each; rows past the end repeat the last one: their results are not stored
+    const uint8_t *pa[TB], *pw[2];
+#pragma unroll
+    for (int x = 0; x < TB; ++x) pa[x] = A + (size_t)min(i0 + x * 64 + (tid >> 2), M - 1) * (K / 2) + (tid & 3) * 16;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) pw[x] = W + (size_t)min(o0 + x * 64 + (tid >> 2), O - 1) * (K / 2) + (tid & 3) * 16;
+    const uint8_t *const pas = As + (size_t)min(i0 + min(tid, kTok - 1), M - 1) * (K / 32);
+    const uint8_t *const pws = Ws + (size_t)min(o0 + (tid & 127), O - 1) * (K / 32);
+    const int at = (tid >> 2) * 64 + (((tid & 3) ^ (tid >> 4)) & 3) * 16;        // place of the first piece; others 64 rows on
+    i32x4 ra[TB], rw[2];
+    uint32_t sca, scw;
+    auto load = [&](int k) {
+#pragma unroll
+        for (int x = 0; x < TB; ++x) ra[x] = *(const i32x4 *)(pa[x] + k / 2);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) rw[x] = *(const i32x4 *)(pw[x] + k / 2);
+        sca = *(const uint32_t *)(pas + k / 32);
+        scw = *(const uint32_t *)(pws + k / 32);
+    };
+    auto store = [&](uint8_t *st) {
+#pragma unroll
+        for (int x = 0; x < TB; ++x) *(i32x4 *)(st + x * 4096 + at) = ra[x];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) *(i32x4 *)(st + kTok * 64 + x * 4096 + at) = rw[x];
+        if (tid < kTok) *(uint32_t *)(st + kRows * 64 + tid * 4) = sca;
+        if (tid < 128) *(uint32_t *)(st + kRows * 64 + (kTok + tid) * 4) = scw;
+    };
+    f32x16 acc[2][TB];
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int b = 0; b < TB; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[a][b][e] = 0.f;
+    auto frag = [&](const uint8_t *st, int row0, int t) {
+        const int r = row0 + l32;
+        const i32x4 u = *(const i32x4 *)(st + r * 64 + (((2 * t + g) ^ (l32 >> 2)) & 3) * 16);
+        return i32x8{u[0], u[1], u[2], u[3], 0, 0, 0, 0};
+    };
+    auto scale = [&](const uint8_t *st, int row0) { return (int)(*(const uint32_t *)(st + kRows * 64 + (row0 + l32) * 4) >> (8 * g)); };
+
+    const int steps = K / 128;
+    load(0);
+    store(smem);
+    __syncthreads();
+    for (int s = 0; s < steps; ++s) {
+        const uint8_t *const st = smem + (s & 1) * kStage;
+        if (s + 1 < steps) load((s + 1) * 128);
+        int sa[TB], sw[2];
+#pragma unroll
+        for (int b = 0; b < TB; ++b) sa[b] = scale(st, wi + 32 * b);
+#pragma unroll
+        for (int a = 0; a < 2; ++a) sw[a] = scale(st, kTok + wo + 32 * a);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            i32x8 wf[2], af[TB];
+#pragma unroll
+            for (int a = 0; a < 2; ++a) wf[a] = frag(st, kTok + wo + 32 * a, t);
+#pragma unroll
+            for (int b = 0; b < TB; ++b) af[b] = frag(st, wi + 32 * b, t);
+#pragma unroll
+            for (int b = 0; b < TB; ++b)
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+                    acc[a][b] = t == 0 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[a], af[b], acc[a][b], kFp4, kFp4, 0, sw[a], 0, sa[b])
+                                       : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[a], af[b], acc[a][b], kFp4, kFp4, 2, sw[a], 2, sa[b]);
+        }
+        if (s + 1 < steps) store(smem + ((s + 1) & 1) * kStage);
+        __syncthreads();
+    }
+
+    // register 4q + r of acc[a][b], lane (l32, g): channel 32 a + 8 q + 4 g + r, token 32 b + l32; v_permlane32_swap brings the
+    // two halves of a 16-byte store together
+    auto swap32 = [](uint32_t &lo, uint32_t &hi) {
+        const auto r = __builtin_amdgcn_permlane32_swap(lo, hi, false, false);
+        lo = r[0];
+        hi = r[1];
+    };
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int q = 0; q < 4; q += 2) {
+            float bi[2][4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) bi[h][r] = bias ? bf16_bits_to_f32(bias[min(o0 + wo + 32 * a + 8 * (q + h) + 4 * g + r, O - 1)]) : 0.f;
+#pragma unroll
+            for (int b = 0; b < TB; ++b) {
+                const int i = i0 + wi + 32 * b + l32, o = o0 + wo + 32 * a + 8 * q + 8 * g;
+                const f32x16 &v = acc[a][b];
+                uint32_t x0 = pack_bf16(v[4 * q] + bi[0][0], v[4 * q + 1] + bi[0][1]), y0 = pack_bf16(v[4 * q + 2] + bi[0][2], v[4 * q + 3] + bi[0][3]);
+                uint32_t x1 = pack_bf16(v[4 * q + 4] + bi[1][0], v[4 * q + 5] + bi[1][1]), y1 = pack_bf16(v[4 * q + 6] + bi[1][2], v[4 * q + 7] + bi[1][3]);
+                swap32(x0, x1);
+                swap32(y0, y1);
+                if (i < M && o < O) *(uint4 *)(Y + (size_t)i * O + o) = make_uint4(x0, y0, x1, y1);      // O is a multiple of 8
+            }
+        }
+}
+
+// Few tokens (at most 16 T): one launch, bound by the weights' bytes and by latency.  A wave takes 16 channels and a part of K
+// in steps of 128: lane l holds the 32 elements 32 (l / 16) .. of row l % 16, one whole block, both of W (as it lies) and of
+// x, which it quantises by itself; no LDS and no exchange between lanes before the waves' sums are added, in order.
+// `parts` waves (a power of two) share 16 channels, 8 / parts groups of channels share a workgroup.
+template <int T>
+__global__ __launch_bounds__(512) void mxfp4_few_kernel(const uint16_t *__restrict__ X, const uint8_t *__restrict__ W, const uint8_t *__restrict__ Ws,
+                                                        const uint16_t *__restrict__ bias, int M, int O, int K, int parts, uint16_t *__restrict__ Y)
+{
+    __shared__ float sums[8][T][16][17];             // [wave][16 tokens][token][channel]
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, r16 = lane & 15, c = lane >> 4;
+    const int part = wave & (parts - 1), group = wave / parts, o0 = ((int)blockIdx.x * (8 / parts) + group) * 16;
+    const int steps = K / 128, per = (steps + parts - 1) / parts, s0 = part * per, s1 = min(steps, s0 + per);
+    const int o = min(o0 + r16, O - 1);              // rows past the end repeat the last one
+    f32x4 acc[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const uint8_t *const w = W + (size_t)o * (K / 2) + c * 16, *const ws = Ws + (size_t)o * (K / 32) + c;
+    const uint16_t *x[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) x[t] = X + (size_t)min(16 * t + r16, M - 1) * K + c * 32;
+    for (int s = s0; s < s1; ++s) {
+        const uint4 u = *(const uint4 *)(w + s * 64);
+        const int sw = ws[s * 4];
+        const i32x8 wf = {(int)u.x, (int)u.y, (int)u.z, (int)u.w, 0, 0, 0, 0};
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            uint4 v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = *(const uint4 *)(x[t] + s * 128 + 8 * q);
+            const uint32_t sx = scale_byte(max(max(top_bits(v[0]), top_bits(v[1])), max(top_bits(v[2]), top_bits(v[3]))));
+            const float scale = scale_value(sx);
+            i32x8 xf = {};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) xf[q] = sx == 255 ? 0 : (int)codes8(v[q], scale);
+            acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf, xf, acc[t], kFp4, kFp4, 0, sw, 0, (int)sx);
+        }
+    }
+    // register r of acc[t]: channel 4 c + r, token 16 t + r16
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sums[wave][t][r16][4 * c + r] = acc[t][r];
+    __syncthreads();
+    const int groups = 8 / parts, out = groups * T * 256;
+    for (int at = threadIdx.x; at < out; at += 512) {
+        const int ch = at & 15, tok = (at >> 4) & 15, t = (at >> 8) % T, gr = (at >> 8) / T;
+        const int oo = ((int)blockIdx.x * groups + gr) * 16 + ch, i = 16 * t + tok;
+        float v = 0.f;
+        for (int p = 0; p < parts; ++p) v += sums[gr * parts + p][t][tok][ch];
+        if (i < M && oo < O) {
+            bf16x2 b;
+            b[0] = (__bf16)(v + (bias ? bf16_bits_to_f32(bias[oo]) : 0.f));
+            Y[(size_t)i * O + oo] = __builtin_bit_cast(uint16_t, b[0]);
+        }
+    }
+}
+
+hipError_t launch_quantise_mxfp4(const void *X, long rows, int cols, void *codes, void *scales, hipStream_t st)
+{
+    const long pieces = rows * (cols / 8), grid = (pieces + 255) / 256;
+    if (grid > 0x7FFFFFFFL) return hipErrorInvalidValue;
+    quantise_mxfp4_kernel<<<(unsigned)grid, 256, 0, st>>>((const uint4 *)X, pieces, (uint32_t *)codes, (uint8_t *)scales);
+    return hipGetLastError();
+}
+
+hipError_t launch_dequantise_mxfp4(const void *codes, const void *scales, long rows, int cols, void *Y, hipStream_t st)
+{
+    const long pieces = rows * (cols / 8), grid = (pieces + 255) / 256;
+    if (grid > 0x7FFFFFFFL) return hipErrorInvalidValue;
+    dequantise_mxfp4_kernel<<<(unsigned)grid, 256, 0, st>>>((const uint32_t *)codes, (const uint8_t *)scales, pieces, (uint4 *)Y);
+    return hipGetLastError();
+}
+
+bool mxfp4_few(int M) { return M <= 32; }
+
+namespace {
+template <int T> hipError_t launch_few(const void *X, const void *W, const void *Ws, const void *bias, int M, int O, int K, void *Y, hipStream_t st)
+{
+    int parts = 1;                                   // waves that share a channel group's K, each with a step at least
+    while (parts < 8 && 2 * parts <= K / 128) parts *= 2;
+    const int channels = 16 * (8 / parts);
+    mxfp4_few_kernel<T><<<(unsigned)((O + channels - 1) / channels), 512, 0, st>>>((const uint16_t *)X, (const uint8_t *)W, (const uint8_t *)Ws,
+                                                                                  (const uint16_t *)bias, M, O, K, parts, (uint16_t *)Y);
+    return hipGetLastError();
+}
+template <int TB>
+hipError_t launch_gemm(const void *A, const void *As, const void *W, const void *Ws, const void *bias, int M, int O, int K, void *Y, hipStream_t st)
+{
+    const int n_it = (M + 64 * TB - 1) / (64 * TB), n_ot = (O + 127) / 128;
+    const long total = (long)n_it * n_ot;
+    if (total > 0x7FFFFFF0L) return hipErrorInvalidValue;
+    mxfp4_gemm_kernel<TB><<<(unsigned)xcd_grid(total), 256, 0, st>>>((const uint8_t *)A, (const uint8_t *)As, (const uint8_t *)W, (const uint8_t *)Ws,
+                                                                     (const uint16_t *)bias, M, O, K, n_ot, (int)total, (uint16_t *)Y);
+    return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_mxfp4_few(const void *X, const void *W, const void *Ws, const void *bias, int M, int O, int K, void *Y, hipStream_t st)
+{
+    if (M <= 16) return launch_few<1>(X, W, Ws, bias, M, O, K, Y, st);
+    return launch_few<2>(X, W, Ws, bias, M, O, K, Y, st);
+}
+
+hipError_t launch_mxfp4_gemm(const void *A, const void *As, const void *W, const void *Ws, const void *bias, int M, int O, int K, void *Y, hipStream_t st)
+{
+    const long n_ot = (O + 127) / 128;
+    if ((M + 255) / 256 * n_ot >= 512) return launch_gemm<4>(A, As, W, Ws, bias, M, O, K, Y, st);
+    if ((M + 127) / 128 * n_ot >= 400) return launch_gemm<2>(A, As, W, Ws, bias, M, O, K, Y, st);
+    return launch_gemm<1>(A, As, W, Ws, bias, M, O, K, Y, st);
+}
+
+}  // namespace sla

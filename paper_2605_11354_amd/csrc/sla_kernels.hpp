@@ -100,6 +100,15 @@ hipError_t launch_linear_dw(const void *dy, const void *x8, const float *sx, int
 // X bf16 [rows, cols] = codes (fragment order) times the scales of their rows
 hipError_t launch_restore_rows(const void *codes, const float *scales, long rows, int cols, void *X, hipStream_t st);
 
+// Microscaled 4-bit numbers (k_mxfp4.hip): codes rows x cols / 2 bytes and scales rows x cols / 32 bytes, cols a multiple of 32
+hipError_t launch_quantise_mxfp4(const void *X, long rows, int cols, void *codes, void *scales, hipStream_t st);
+hipError_t launch_dequantise_mxfp4(const void *codes, const void *scales, long rows, int cols, void *Y, hipStream_t st);
+// Y bf16 [M,O] = A [M,K] W [O,K]^T + bias of two matrices in that form, K a multiple of 128, O of 8; bias may be NULL
+hipError_t launch_mxfp4_gemm(const void *A, const void *As, const void *W, const void *Ws, const void *bias, int M, int O, int K, void *Y, hipStream_t st);
+// the same for few rows of bf16 X, quantised on the way (no workspace)
+bool mxfp4_few(int M);
+hipError_t launch_mxfp4_few(const void *X, const void *W, const void *Ws, const void *bias, int M, int O, int K, void *Y, hipStream_t st);
+
 // Norm and rotation of the heads of a projection's output (k_heads.hip).  Strides in elements; x and y [0..2] = q, k, v.
 struct HeadsArgs {
     const uint16_t *x[3];       // inputs, row (b, t, h) at b bs + t ts + h hs

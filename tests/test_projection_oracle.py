@@ -54,3 +54,28 @@ def test_gradients_are_the_difference_quotients(norm, axes, pairing):
             continue
         way = rng.standard_normal(t.shape)
         assert abs((call(t + h * way) - call(t - h * way)) / (2 * h) - float((grad * way).sum())) < 1e-6 * max(1.0, abs(float((grad * way).sum())))
+
+
+def test_mxfp4_of_known_blocks():
+    row = np.zeros(32)
+    row[:8] = [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 4.0]                    # the ties, at scale 1
+    c, s = po.mxfp4_quantise((row.astype(np.float32).view(np.uint32) >> 16).astype(np.uint16)[None])
+    assert s.tolist() == [[127]] and c[0, :8].tolist() == [0, 2, 2, 4, 4, 6, 6, 6]
+    row[:8] = [7.5, -7.5, -0.25, 0.24, -6.0, 5.1, -0.0, 1.0]
+    c, s = po.mxfp4_quantise((row.astype(np.float32).view(np.uint32) >> 16).astype(np.uint16)[None])
+    assert s.tolist() == [[127]] and c[0, :8].tolist() == [7, 15, 8, 0, 15, 7, 8, 2]
+    assert po.mxfp4_values(c, s)[0, :8].tolist() == [6.0, -6.0, 0.0, 0.0, -6.0, 6.0, 0.0, 1.0]
+    c, s = po.mxfp4_quantise(np.zeros((1, 64), np.uint16))
+    assert s.tolist() == [[0, 0]] and not c.any()
+
+
+def test_mxfp4_scale_is_a_power_of_two_and_the_error_at_most_a_step():
+    rng = np.random.default_rng(3)
+    x = (rng.standard_normal((20, 96)) * np.exp(rng.uniform(-80, 80, (20, 1)))).astype(np.float32)
+    bits = (x.view(np.uint32) >> 16).astype(np.uint16)
+    c, s = po.mxfp4_quantise(bits)
+    x = po.bf16_to_f64(bits)
+    top = np.abs(x.reshape(20, 3, 32)).max(-1)
+    # the largest element is below 8 scales and comes out as 4 or 6 of them (3.5 upwards rounds to 4)
+    assert (top < 8 * np.ldexp(1.0, s - 127)).all() and (top >= 4 * np.ldexp(1.0, s - 127)).all()
+    assert (np.abs(po.mxfp4_values(c, s) - x) <= np.repeat(2 * np.ldexp(1.0, s - 127), 32, 1)).all()
