@@ -25,6 +25,14 @@ EXPORTS = ["sla_resolve_counts", "sla_workspace_bytes", "sla_forward", "sla_pool
            "sla_quantise_mxfp4", "sla_dequantise_mxfp4", "sla_mxfp4_linear_workspace_bytes", "sla_mxfp4_linear",
            "sla_qk_norm_rope", "sla_qk_norm_rope_e4m3", "sla_qk_norm_rope_grad_workspace_bytes", "sla_qk_norm_rope_grad",
            "sla_strerror", "sla_last_error", "sla_stage_name"]
+# argument kinds of the calls that a decoding step or a short layer makes often: pointer, int32, int64, size_t
+_KINDS = {"p": C.c_void_p, "i": C.c_int32, "l": C.c_int64, "z": C.c_size_t}
+_ARGUMENTS = {"sla_qk_norm_rope": "p" * 13, "sla_qk_norm_rope_e4m3": "p" * 9 + "i" + "p" * 7, "sla_qk_norm_rope_grad": "p" * 17 + "zp",
+              "sla_qk_norm_rope_grad_workspace_bytes": "pp",
+              "sla_fp8_checkpoint_bytes": "iip", "sla_fp8_checkpoint_restore": "pziipp", "sla_fp8_linear_grad_workspace_bytes": "iiip",
+              "sla_fp8_linear_save": "pppiiippzpzp", "sla_fp8_linear_grad": "ppzpiiippppzp",
+              "sla_quantise_mxfp4": "plippp", "sla_dequantise_mxfp4": "pplipp", "sla_mxfp4_linear_workspace_bytes": "iiip",
+              "sla_mxfp4_linear": "ppppiiippzp"}
 STATIC_WORKSPACE_BYTES = 96 * 1024 * 1024
 NUM_STAGES = 6
 
@@ -60,6 +68,8 @@ def lib() -> C.CDLL:
         _lib.sla_strerror.restype = C.c_char_p
         _lib.sla_last_error.restype = C.c_char_p
         _lib.sla_stage_name.restype = C.c_char_p
+        for name, kinds in _ARGUMENTS.items():       # with these, plain integers and None pass for pointers and sizes
+            getattr(_lib, name).argtypes = [_KINDS[k] for k in kinds]
         for name in EXPORTS[:-3]:                    # all but the three that return text
             getattr(_lib, name).restype = C.c_int
     return _lib
@@ -223,6 +233,47 @@ def sla_fp8_linear_qkv(x, W, bias, B_, N, H, bq, Q8, K8, V8, sQ, sK, sV, workspa
                                     _ptr(workspace), C.c_size_t(workspace.numel()), _stream()), "sla_fp8_linear_qkv")
 
 
+# ---- what the calls below share: checks of tensors against the sizes that go with the pointers
+def _device() -> int:
+    """The current device; before any is in use there are no device tensors, and every tensor is refused."""
+    return torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+
+
+def _raw_stream(dev):
+    return torch._C._cuda_getCurrentRawStream(dev)       # torch.cuda.current_stream().cuda_stream without the object around it
+
+
+def _refuse(t, what, dtype, shape, dev):
+    if t.dtype != dtype or tuple(t.shape) != shape:
+        raise ValueError(f"{what}: {dtype} {list(shape)} expected, got {t.dtype} {list(t.shape)}")
+    raise ValueError(f"{what}: a contiguous tensor on the current device expected, got one on {t.device} with strides {list(t.stride())}")
+
+
+def _tensor(t, what, dtype, shape, dev):
+    """Pointer of a dense device tensor of this type and shape (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        _refuse(t, what, dtype, shape, dev)
+    return t.data_ptr()
+
+
+def _buffer(t, what, dev):
+    """(pointer, bytes) of a checkpoint or workspace."""
+    n = t.numel()
+    return _tensor(t, what, torch.uint8, (n,), dev), n
+
+
+def _bytes(name, *sizes) -> int:
+    n = C.c_size_t()
+    _check(getattr(lib(), name)(*sizes, C.byref(n)), name)
+    return n.value
+
+
+def _scratch(need, device):
+    return torch.empty(max(256, need), dtype=torch.uint8, device=device)
+
+
 # ---- norm and rotation of heads
 class SlaHeadsParams(C.Structure):
     _fields_ = [("B", C.c_int32), ("H", C.c_int32), ("N", C.c_int32), ("D", C.c_int32),
@@ -243,93 +294,77 @@ def make_heads_params(q, norm="layer", norm_per_head=False, eps=1e-5, axes=2, pa
                           q.stride(0), q.stride(1), q.stride(2))
 
 
-def _tensor(t, what, dtype, shape):
-    """Pointer of a dense device tensor of this type and shape (None: NULL)."""
-    if t is None:
-        return None
-    if t.dtype != dtype or tuple(t.shape) != shape:
-        raise ValueError(f"{what}: {dtype} {list(shape)} expected, got {t.dtype} {list(t.shape)}")
-    if not t.is_cuda or t.device.index != torch.cuda.current_device() or not t.is_contiguous():
-        raise ValueError(f"{what}: a contiguous tensor on the current device expected")
-    return t.data_ptr()
+class _Heads:
+    """The sizes in p as the tensors of a call have to have them."""
 
+    def __init__(self, p):
+        self.p, self.dev = p, _device()
+        self.shape = (p.B, p.N, p.H, p.D)
+        self.strides = (p.batch_stride, p.token_stride, p.head_stride, 1)
+        self.out = self.shape if p.layout else (p.B, p.H, p.N, p.D)
 
-def _rows(p, t, what):
-    """Pointer of a [B,N,H,64] tensor with the strides in p."""
-    if t is None:
-        return None
-    shape, strides = (p.B, p.N, p.H, p.D), (p.batch_stride, p.token_stride, p.head_stride, 1)
-    if t.dtype != torch.bfloat16 or tuple(t.shape) != shape or any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), strides)):
-        raise ValueError(f"{what}: bfloat16 {list(shape)} with strides {list(strides)} expected, got {t.dtype} {list(t.shape)} {list(t.stride())}")
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{what}: a tensor on the current device expected")
-    return t.data_ptr()
+    def rows(self, t, what):
+        """Pointer of a [B,N,H,64] tensor with the strides in p."""
+        if t is None:
+            return None
+        if t.dtype is not torch.bfloat16 or t.shape != self.shape or t.get_device() != self.dev or \
+                (t.stride() != self.strides and any(n > 1 and a != b for n, a, b in zip(self.shape, t.stride(), self.strides))):
+            raise ValueError(f"{what}: bfloat16 {list(self.shape)} with strides {list(self.strides)} on the current device "
+                             f"expected, got {t.dtype} {list(t.shape)} {list(t.stride())} on {t.device}")
+        return t.data_ptr()
 
+    def dense(self, t, what, dtype=torch.bfloat16):
+        return _tensor(t, what, dtype, self.out, self.dev)
 
-def _heads_parameters(p, pos, *params):
-    shape = (p.H, 64) if p.norm_per_head else (64,)
-    names = ("q_weight", "q_bias", "k_weight", "k_bias")
-    ptrs = [_tensor(t, n, torch.float32, shape) for t, n in zip(params, names)]
-    full = (p.B if p.pos_per_item else 1, p.N, p.axes)
-    return ptrs, _tensor(pos, "pos", torch.int32, full[1:] if pos is not None and pos.dim() == 2 and full[0] == 1 else full)
+    def weight(self, t, what):
+        return _tensor(t, what, torch.float32, (self.p.H, 64) if self.p.norm_per_head else (64,), self.dev) if t is not None else None
 
-
-def _heads_shape(p):
-    return (p.B, p.N, p.H, 64) if p.layout else (p.B, p.H, p.N, 64)
-
-
-def _ptrs(ptrs):
-    return [C.c_void_p(x) for x in ptrs]
+    def positions(self, pos):
+        if pos is None:
+            return None
+        full = (self.p.B if self.p.pos_per_item else 1, self.p.N, self.p.axes)
+        return _tensor(pos, "pos", torch.int32, full[1:] if pos.dim() == 2 and full[0] == 1 else full, self.dev)
 
 
 def sla_qk_norm_rope(p, q, k, v, Q, K, V, pos=None, q_weight=None, q_bias=None, k_weight=None, k_bias=None):
     """q, k, v bf16 [B,N,H,64] in the strides of p -> Q, K, V bf16 in p's layout; pos int32 [N,axes], [1,N,axes] or [B,N,axes]."""
-    w, at = _heads_parameters(p, pos, q_weight, q_bias, k_weight, k_bias)
-    shape = _heads_shape(p)
-    args = [_rows(p, q, "q"), _rows(p, k, "k"), _rows(p, v, "v"), *w, at, *(_tensor(t, n, torch.bfloat16, shape) for t, n in zip((Q, K, V), "QKV"))]
-    _check(lib().sla_qk_norm_rope(C.byref(p), *_ptrs(args), _stream()), "sla_qk_norm_rope")
+    h = _Heads(p)
+    _check(lib().sla_qk_norm_rope(C.byref(p), h.rows(q, "q"), h.rows(k, "k"), h.rows(v, "v"), h.weight(q_weight, "q_weight"), h.weight(q_bias, "q_bias"),
+                                  h.weight(k_weight, "k_weight"), h.weight(k_bias, "k_bias"), h.positions(pos),
+                                  h.dense(Q, "Q"), h.dense(K, "K"), h.dense(V, "V"), _raw_stream(h.dev)), "sla_qk_norm_rope")
     return Q, K, V
 
 
 def sla_qk_norm_rope_e4m3(p, q, k, v, bq, Q8, K8, V8, sQ, sK, sV, pos=None, q_weight=None, q_bias=None, k_weight=None, k_bias=None):
     """The same into E4M3 codes (uint8, p's layout) with block scales fp32 [B,H,ceil(N/bq)], [B,H,ceil(N/64)] twice."""
-    w, at = _heads_parameters(p, pos, q_weight, q_bias, k_weight, k_bias)
-    shape, blocks = _heads_shape(p), [(p.B, p.H, -(-p.N // max(b, 1))) for b in (bq, 64, 64)]
-    args = [_rows(p, q, "q"), _rows(p, k, "k"), _rows(p, v, "v"), *w, at]
-    out = [_tensor(t, n, torch.uint8, shape) for t, n in zip((Q8, K8, V8), ("Q8", "K8", "V8"))]
-    out += [_tensor(t, n, torch.float32, s) for t, n, s in zip((sQ, sK, sV), ("sQ", "sK", "sV"), blocks)]
-    _check(lib().sla_qk_norm_rope_e4m3(C.byref(p), *_ptrs(args), C.c_int32(bq), *_ptrs(out), _stream()), "sla_qk_norm_rope_e4m3")
+    h, u8 = _Heads(p), torch.uint8
+    scales = lambda t, what, blk: _tensor(t, what, torch.float32, (p.B, p.H, -(-p.N // max(blk, 1))), h.dev)
+    _check(lib().sla_qk_norm_rope_e4m3(C.byref(p), h.rows(q, "q"), h.rows(k, "k"), h.rows(v, "v"), h.weight(q_weight, "q_weight"), h.weight(q_bias, "q_bias"),
+                                       h.weight(k_weight, "k_weight"), h.weight(k_bias, "k_bias"), h.positions(pos), bq,
+                                       h.dense(Q8, "Q8", u8), h.dense(K8, "K8", u8), h.dense(V8, "V8", u8),
+                                       scales(sQ, "sQ", bq), scales(sK, "sK", 64), scales(sV, "sV", 64), _raw_stream(h.dev)), "sla_qk_norm_rope_e4m3")
     return Q8, K8, V8, sQ, sK, sV
 
 
 def sla_qk_norm_rope_grad_workspace_bytes(p) -> int:
-    n = C.c_size_t()
-    _check(lib().sla_qk_norm_rope_grad_workspace_bytes(C.byref(p), C.byref(n)), "sla_qk_norm_rope_grad_workspace_bytes")
-    return n.value
+    return _bytes("sla_qk_norm_rope_grad_workspace_bytes", C.byref(p))
 
 
 def sla_qk_norm_rope_grad(p, q, k, dQ, dK, dV, dq, dk, dv, pos=None, q_weight=None, k_weight=None, dq_weight=None, dq_bias=None,
                           dk_weight=None, dk_bias=None, workspace=None):
     """dQ, dK, dV (bf16, p's layout) -> dq, dk, dv (bf16, the strides of q, k, v) and fp32 gradients of the norm's parameters."""
-    w, at = _heads_parameters(p, pos, q_weight, None, k_weight, None)
-    dw, _ = _heads_parameters(p, None, dq_weight, dq_bias, dk_weight, dk_bias)
-    shape = _heads_shape(p)
+    h = _Heads(p)
     if workspace is None:
-        workspace = torch.empty(max(256, sla_qk_norm_rope_grad_workspace_bytes(p)), dtype=torch.uint8, device=q.device)
-    args = [_rows(p, q, "q"), _rows(p, k, "k"), w[0], w[2], at, *(_tensor(t, n, torch.bfloat16, shape) for t, n in zip((dQ, dK, dV), ("dQ", "dK", "dV"))),
-            _rows(p, dq, "dq"), _rows(p, dk, "dk"), _rows(p, dv, "dv"), *dw]
-    _check(lib().sla_qk_norm_rope_grad(C.byref(p), *_ptrs(args), _ptr(workspace), C.c_size_t(workspace.numel()), _stream()),
-           "sla_qk_norm_rope_grad")
+        workspace = _scratch(sla_qk_norm_rope_grad_workspace_bytes(p), q.device)
+    _check(lib().sla_qk_norm_rope_grad(C.byref(p), h.rows(q, "q"), h.rows(k, "k"), h.weight(q_weight, "q_weight"), h.weight(k_weight, "k_weight"),
+                                       h.positions(pos), h.dense(dQ, "dQ"), h.dense(dK, "dK"), h.dense(dV, "dV"),
+                                       h.rows(dq, "dq"), h.rows(dk, "dk"), h.rows(dv, "dv"), h.weight(dq_weight, "dq_weight"), h.weight(dq_bias, "dq_bias"),
+                                       h.weight(dk_weight, "dk_weight"), h.weight(dk_bias, "dk_bias"), *_buffer(workspace, "workspace", h.dev),
+                                       _raw_stream(h.dev)), "sla_qk_norm_rope_grad")
     return dq, dk, dv
 
 
 # ---- training of the FP8 layer from an 8-bit copy of its input
-def _bytes(name, *sizes) -> int:
-    n = C.c_size_t()
-    _check(getattr(lib(), name)(*[C.c_int32(x) for x in sizes], C.byref(n)), name)
-    return n.value
-
-
 def sla_fp8_checkpoint_bytes(N, d_in) -> int:
     return _bytes("sla_fp8_checkpoint_bytes", N, d_in)
 
@@ -338,62 +373,50 @@ def sla_fp8_linear_grad_workspace_bytes(N, d_in, d_out) -> int:
     return _bytes("sla_fp8_linear_grad_workspace_bytes", N, d_in, d_out)
 
 
-def _buffer(t, what):
-    """(pointer, bytes) of a checkpoint or workspace."""
-    p = _tensor(t, what, torch.uint8, (t.numel(),))
-    return C.c_void_p(p), C.c_size_t(t.numel())
-
-
-def _linear_workspace(workspace, N, d_in, d_out, device):
-    if workspace is None:
-        workspace = torch.empty(max(256, sla_fp8_linear_grad_workspace_bytes(N, d_in, d_out)), dtype=torch.uint8, device=device)
-    return _buffer(workspace, "workspace")
-
-
 def sla_fp8_linear_save(x, W, bias, y, checkpoint, workspace=None):
     """sla_fp8_linear that leaves x in 8 bits in `checkpoint` (uint8, sla_fp8_checkpoint_bytes(N, d_in) long)."""
-    (N, d_in), d_out, bf = x.shape, W.shape[0], torch.bfloat16
-    args = _ptrs([_tensor(x, "x", bf, (N, d_in)), _tensor(W, "W", bf, (d_out, d_in)), _tensor(bias, "bias", bf, (d_out,))])
-    _check(lib().sla_fp8_linear_save(*args, C.c_int32(N), C.c_int32(d_in), C.c_int32(d_out), C.c_void_p(_tensor(y, "y", bf, (N, d_out))),
-                                     *_buffer(checkpoint, "checkpoint"), *_linear_workspace(workspace, N, d_in, d_out, x.device), _stream()),
-           "sla_fp8_linear_save")
+    (N, d_in), d_out, bf, dev = x.shape, W.shape[0], torch.bfloat16, _device()
+    if workspace is None:
+        workspace = _scratch(sla_fp8_linear_grad_workspace_bytes(N, d_in, d_out), x.device)
+    _check(lib().sla_fp8_linear_save(_tensor(x, "x", bf, (N, d_in), dev), _tensor(W, "W", bf, (d_out, d_in), dev), _tensor(bias, "bias", bf, (d_out,), dev),
+                                     N, d_in, d_out, _tensor(y, "y", bf, (N, d_out), dev), *_buffer(checkpoint, "checkpoint", dev),
+                                     *_buffer(workspace, "workspace", dev), _raw_stream(dev)), "sla_fp8_linear_save")
     return y
 
 
 def sla_fp8_linear_grad(dy, checkpoint, W, dx=None, dW=None, db=None, workspace=None):
     """Gradients of sla_fp8_linear_save's x, W and bias (each may be None; db only with dW) from that of its y."""
-    (N, d_out), d_in, bf = dy.shape, W.shape[1], torch.bfloat16
-    out = _ptrs([_tensor(dx, "dx", bf, (N, d_in)), _tensor(dW, "dW", bf, (d_out, d_in)), _tensor(db, "db", bf, (d_out,))])
-    _check(lib().sla_fp8_linear_grad(C.c_void_p(_tensor(dy, "dy", bf, (N, d_out))), *_buffer(checkpoint, "checkpoint"),
-                                     C.c_void_p(_tensor(W, "W", bf, (d_out, d_in))), C.c_int32(N), C.c_int32(d_in), C.c_int32(d_out), *out,
-                                     *_linear_workspace(workspace, N, d_in, d_out, dy.device), _stream()), "sla_fp8_linear_grad")
+    (N, d_out), d_in, bf, dev = dy.shape, W.shape[1], torch.bfloat16, _device()
+    if workspace is None:
+        workspace = _scratch(sla_fp8_linear_grad_workspace_bytes(N, d_in, d_out), dy.device)
+    _check(lib().sla_fp8_linear_grad(_tensor(dy, "dy", bf, (N, d_out), dev), *_buffer(checkpoint, "checkpoint", dev), _tensor(W, "W", bf, (d_out, d_in), dev),
+                                     N, d_in, d_out, _tensor(dx, "dx", bf, (N, d_in), dev), _tensor(dW, "dW", bf, (d_out, d_in), dev),
+                                     _tensor(db, "db", bf, (d_out,), dev), *_buffer(workspace, "workspace", dev), _raw_stream(dev)), "sla_fp8_linear_grad")
     return dx, dW, db
 
 
 def sla_fp8_checkpoint_restore(checkpoint, x):
     """x bf16 [N,d_in] <- the layer's input as its forward multiplied it."""
-    N, d_in = x.shape
-    _check(lib().sla_fp8_checkpoint_restore(*_buffer(checkpoint, "checkpoint"), C.c_int32(N), C.c_int32(d_in),
-                                            C.c_void_p(_tensor(x, "x", torch.bfloat16, (N, d_in))), _stream()), "sla_fp8_checkpoint_restore")
+    (N, d_in), dev = x.shape, _device()
+    _check(lib().sla_fp8_checkpoint_restore(*_buffer(checkpoint, "checkpoint", dev), N, d_in, _tensor(x, "x", torch.bfloat16, (N, d_in), dev),
+                                            _raw_stream(dev)), "sla_fp8_checkpoint_restore")
     return x
 
 
 # ---- microscaled 4-bit numbers
 def sla_quantise_mxfp4(X, codes, scales):
     """X bf16 [rows, cols] -> codes uint8 [rows, cols/2], scales uint8 [rows, cols/32]."""
-    rows, cols = X.shape
-    args = _ptrs([_tensor(codes, "codes", torch.uint8, (rows, cols // 2)), _tensor(scales, "scales", torch.uint8, (rows, cols // 32))])
-    _check(lib().sla_quantise_mxfp4(C.c_void_p(_tensor(X, "X", torch.bfloat16, (rows, cols))), C.c_int64(rows), C.c_int32(cols), *args, _stream()),
-           "sla_quantise_mxfp4")
+    (rows, cols), u8, dev = X.shape, torch.uint8, _device()
+    _check(lib().sla_quantise_mxfp4(_tensor(X, "X", torch.bfloat16, (rows, cols), dev), rows, cols, _tensor(codes, "codes", u8, (rows, cols // 2), dev),
+                                    _tensor(scales, "scales", u8, (rows, cols // 32), dev), _raw_stream(dev)), "sla_quantise_mxfp4")
     return codes, scales
 
 
 def sla_dequantise_mxfp4(codes, scales, Y):
     """Y bf16 [rows, cols] <- the numbers that codes and scales stand for."""
-    rows, cols = Y.shape
-    args = _ptrs([_tensor(codes, "codes", torch.uint8, (rows, cols // 2)), _tensor(scales, "scales", torch.uint8, (rows, cols // 32))])
-    _check(lib().sla_dequantise_mxfp4(*args, C.c_int64(rows), C.c_int32(cols), C.c_void_p(_tensor(Y, "Y", torch.bfloat16, (rows, cols))), _stream()),
-           "sla_dequantise_mxfp4")
+    (rows, cols), u8, dev = Y.shape, torch.uint8, _device()
+    _check(lib().sla_dequantise_mxfp4(_tensor(codes, "codes", u8, (rows, cols // 2), dev), _tensor(scales, "scales", u8, (rows, cols // 32), dev),
+                                      rows, cols, _tensor(Y, "Y", torch.bfloat16, (rows, cols), dev), _raw_stream(dev)), "sla_dequantise_mxfp4")
     return Y
 
 
@@ -403,11 +426,11 @@ def sla_mxfp4_linear_workspace_bytes(N, d_in, d_out) -> int:
 
 def sla_mxfp4_linear(x, W_codes, W_scales, bias, y, workspace=None):
     """y bf16 [N,d_out] <- linear layer of x bf16 [N,d_in], both factors in microscaled 4-bit numbers."""
-    (N, d_in), d_out, bf = x.shape, W_codes.shape[0], torch.bfloat16
-    args = _ptrs([_tensor(x, "x", bf, (N, d_in)), _tensor(W_codes, "W_codes", torch.uint8, (d_out, d_in // 2)),
-                  _tensor(W_scales, "W_scales", torch.uint8, (d_out, d_in // 32)), _tensor(bias, "bias", bf, (d_out,))])
+    (N, d_in), d_out, bf, u8, dev = x.shape, W_codes.shape[0], torch.bfloat16, torch.uint8, _device()
     if workspace is None:
-        workspace = torch.empty(max(256, sla_mxfp4_linear_workspace_bytes(N, d_in, d_out)), dtype=torch.uint8, device=x.device)
-    _check(lib().sla_mxfp4_linear(*args, C.c_int32(N), C.c_int32(d_in), C.c_int32(d_out), C.c_void_p(_tensor(y, "y", bf, (N, d_out))),
-                                  *_buffer(workspace, "workspace"), _stream()), "sla_mxfp4_linear")
+        workspace = _scratch(sla_mxfp4_linear_workspace_bytes(N, d_in, d_out), x.device)
+    _check(lib().sla_mxfp4_linear(_tensor(x, "x", bf, (N, d_in), dev), _tensor(W_codes, "W_codes", u8, (d_out, d_in // 2), dev),
+                                  _tensor(W_scales, "W_scales", u8, (d_out, d_in // 32), dev), _tensor(bias, "bias", bf, (d_out,), dev),
+                                  N, d_in, d_out, _tensor(y, "y", bf, (N, d_out), dev), *_buffer(workspace, "workspace", dev), _raw_stream(dev)),
+           "sla_mxfp4_linear")
     return y

@@ -234,3 +234,20 @@ def test_replays_from_a_graph_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, outs)), k
+
+
+def test_tensors_of_another_shape_type_or_place_are_refused():
+    h = Heads(2, 5, 3)
+    out, bad = h.out(), torch.empty(32, device="cuda")
+    pos = lambda *shape, dtype=torch.int32: torch.zeros(shape, dtype=dtype, device="cuda")
+    for name, kw in [("q_weight", dict(q_weight=bad)), ("k_bias", dict(k_bias=torch.empty(64))), ("pos", dict(pos=pos(5, 1))), ("pos", dict(pos=pos(2, 5, 2))),
+                     ("pos", dict(pos=pos(5, 2, dtype=torch.int64)))]:
+        with pytest.raises(ValueError, match=name):
+            B.sla_qk_norm_rope(h.p, *h.x, *out, **kw)
+    with pytest.raises(ValueError, match="K: "):
+        B.sla_qk_norm_rope(h.p, *h.x, out[0], out[1][:, :, :4], out[2], pos=h.pos)
+    with pytest.raises(ValueError, match="k: "):
+        B.sla_qk_norm_rope(h.p, h.x[0], h.x[1].float(), h.x[2], *out, pos=h.pos)
+    h.p.pos_per_item = 1
+    with pytest.raises(ValueError, match="pos"):                                             # two items, positions of one
+        B.sla_qk_norm_rope(h.p, *h.x, *out, pos=h.pos)

@@ -140,3 +140,15 @@ def test_replays_from_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a.view(torch.int16), c.view(torch.int16)) for a, c in zip(want, (y, dx, dW, db))), k
+
+
+def test_tensors_of_another_shape_type_or_place_are_refused():
+    ck, ws, y, dx, dW, db = buffers(5, 128, 8)
+    W, x = dW.clone(), dx.clone()
+    for name, kw in [("dx", dict(dx=dx[:4])), ("db", dict(dW=dW, db=db[:4])), ("dW", dict(dW=dW.cpu())), ("workspace", dict(workspace=ws.float()))]:
+        with pytest.raises(ValueError, match=name):
+            B.sla_fp8_linear_grad(y, ck, W, **kw)
+    with pytest.raises(ValueError, match="y: "):
+        B.sla_fp8_linear_save(x, W, None, y.t(), ck)
+    with pytest.raises(B.SlaError, match="checkpoint has"):
+        B.sla_fp8_linear_grad(y, ck[:256], W, dW=dW)

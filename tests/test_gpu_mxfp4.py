@@ -155,3 +155,13 @@ def test_replays_from_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(want[0].view(torch.int16), y.view(torch.int16)) and torch.equal(want[1].view(torch.int16), z.view(torch.int16)), k
+
+
+def test_tensors_of_another_shape_type_or_place_are_refused():
+    x, c, s = torch.empty((4, 128), dtype=torch.bfloat16, device="cuda"), torch.empty((8, 64), dtype=torch.uint8, device="cuda"), torch.empty((8, 4), dtype=torch.uint8, device="cuda")
+    with pytest.raises(ValueError, match="codes"):
+        B.sla_quantise_mxfp4(x, c, s)
+    with pytest.raises(ValueError, match="W_scales"):
+        B.sla_mxfp4_linear(x, c, s[:, :2], None, x[:, :8].contiguous())
+    with pytest.raises(ValueError, match="y: "):
+        B.sla_mxfp4_linear(x, c, s, None, x[:, :8])

@@ -79,7 +79,7 @@ def test_nothing_to_do(lib, kw):
     p = params(**kw)
     assert lib.sla_qk_norm_rope(C.byref(p), *[NULL] * 12) == B.SLA_OK
     assert lib.sla_qk_norm_rope_e4m3(C.byref(p), *[NULL] * 8, C.c_int32(64), *[NULL] * 7) == B.SLA_OK
-    assert lib.sla_qk_norm_rope_grad(C.byref(p), *[NULL] * 15, C.c_size_t(0), NULL) == B.SLA_OK
+    assert lib.sla_qk_norm_rope_grad(C.byref(p), *[NULL] * 16, C.c_size_t(0), NULL) == B.SLA_OK
     assert B.sla_qk_norm_rope_grad_workspace_bytes(p) == 0
 
 
@@ -97,10 +97,3 @@ def test_tensors_of_another_shape_or_type():
         B.sla_qk_norm_rope(p, q, q, q, *out, pos=None)
     with pytest.raises(ValueError, match="strides"):
         B.sla_qk_norm_rope(p, q.contiguous(), q, q, *out)
-    with pytest.raises(ValueError, match="q_weight"):
-        B.sla_qk_norm_rope(p, q, q, q, *out, q_weight=torch.empty(32))
-    with pytest.raises(ValueError, match="pos"):
-        B.sla_qk_norm_rope(p, q, q, q, *out, pos=torch.empty((5, 1), dtype=torch.int32))
-    p.pos_per_item = 1
-    with pytest.raises(ValueError, match="pos"):                                             # two items, positions of one
-        B.sla_qk_norm_rope(p, q, q, q, *out, pos=torch.empty((5, 2), dtype=torch.int32))

@@ -62,8 +62,6 @@ def test_nothing_to_do(lib):
 def test_tensors_of_another_shape_type_or_place():
     bf, u8 = torch.bfloat16, torch.uint8
     x, c, s = torch.empty((4, 128), dtype=bf), torch.empty((8, 64), dtype=u8), torch.empty((8, 4), dtype=u8)
-    with pytest.raises(ValueError, match="codes"):
-        B.sla_quantise_mxfp4(x, c, s)
     with pytest.raises(ValueError, match="current device"):
         B.sla_quantise_mxfp4(x, c[:4], s[:4])
     with pytest.raises(ValueError, match="x: "):
