@@ -19,6 +19,9 @@ SOURCES = ["sla_api.hip", "k_classify.hip", "k_states.hip", "k_aggregate.hip", "
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-ffp-contract=off", "-Wall", "-Wextra",
          "-Wno-unused-parameter", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-mllvm", "-amdgpu-mfma-vgpr-form=1"]   # MFMA accumulators stay in VGPRs: no AGPR copy traffic
+# The wide tiles of this file hold 256 accumulators a lane, which only the other half of the register file has room for (with
+# the flag its main loop copies two hundred registers a step)
+AGPR_FORM = ["k_linear_grad.hip"]
 
 
 def _hipcc() -> str:
@@ -31,7 +34,8 @@ def _hipcc() -> str:
 def _compile(job) -> str:
     src, probe = job if isinstance(job, tuple) else (job, False)
     obj = os.path.join(OBJ, ("probe_" if probe else "") + src.replace(".hip", ".o"))
-    cmd = [_hipcc(), *FLAGS, *(["-DSLA_PROBE_TIME"] if probe else []), "-c", os.path.join(CSRC, src), "-o", obj]
+    flags = FLAGS[:-2] if src in AGPR_FORM else FLAGS
+    cmd = [_hipcc(), *flags, *(["-DSLA_PROBE_TIME"] if probe else []), "-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     err = "\n".join(l for l in r.stderr.splitlines() if "packed-fp32-ops" not in l)
     if r.returncode != 0:

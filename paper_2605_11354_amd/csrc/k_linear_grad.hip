@@ -5,10 +5,15 @@
 //     db = sum over tokens of dy
 // x is kept for the backward pass as those codes and one fp32 scale per token: N (d_in + 4) bytes instead of 2 N d_in.
 //
-// Both products have one form: C[m][n] = sum_k A(m,k) B(k,n), with B the code matrix (rows k = channels of W or tokens of x, in the
-// fragment order of k_linear.hip) times the scale of the row, rounded to bf16, and A = dy, read as it lies (dx) or transposed (dW).
-// The scale belongs to the summation index, so it cannot wait for the epilogue.  Rounding code x scale to bf16 is off by at
-// most 2^-8 of it, as the rounding of x to bf16 was in the first place; products are exact in the fp32 accumulators.
+// Both products have one form: C[m][n] = sum_k A(m,k) B(k,n), with B the code matrix (rows k = channels of W or tokens of x) times the
+// scale of the row, rounded to bf16, and A = dy, read as it lies (dx) or transposed (dW).  The scale belongs to the summation
+// index, so it cannot wait for the epilogue.  Rounding code x scale to bf16 is off by at most 2^-8 of it, as the rounding of x to bf16
+// was in the first place; products are exact in the fp32 accumulators.
+//
+// B is restored once, by restore_turned_kernel, into the order in which the matrix unit's operands are read: column groups of 32, of
+// a group 16 k after 16 k, 1 KB each, lane l's 16 bytes (column l % 32, k = 8 (l / 32) ..) one after the other; k past the end are
+// zeros up to a multiple of 32.  (Converted on the way to LDS instead, every tile of rows converts it again: four vector instructions
+// for each matrix instruction, 540 us instead of 30 for the restoring and what the products then take.)
 #include "sla_common.hpp"
 #include "sla_kernels.hpp"
 
@@ -17,7 +22,7 @@
 namespace sla {
 
 namespace {
-constexpr int kStepK = 32;                           // summation indices of a step: one group of rows of the code matrix
+constexpr int kStepK = 32;                           // summation indices of a step
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 
 // Tiles that lie [k][column] in LDS: a row is 2 columns bytes, its 16-byte piece c at position c ^ swizzle(k).  Four
@@ -25,7 +30,7 @@ typedef __attribute__((ext_vector_type(4))) short s16x4;
 // four rows at a time), and writes of one piece by consecutive k go to sixteen different places.
 __device__ __forceinline__ int swizzle(int k) { return 4 * (k & 3) | ((k >> 2) & 3); }
 
-// MFMA operand of 32 columns n0 .. n0 + 31 and the 16 indices of step t from a tile that lies [k][column]: lane l gets column
+// MFMA operand of 32 columns n0 .. n0 + 31 and the 16 indices of part t from a tile that lies [k][column]: lane l gets column
 // l % 32, k = 16 t + 8 (l / 32) .. + 7.  Each ds_read_b64_tr_b16 turns, in every 16 lanes, 4 rows x 16 columns around.
 template <int COLS> __device__ __forceinline__ bf16x8 read_turned(const uint8_t *tile, int n0, int t, int lane)
 {
@@ -41,88 +46,114 @@ template <int COLS> __device__ __forceinline__ bf16x8 read_turned(const uint8_t 
 }
 
 // sixteen E4M3 codes times a scale, rounded to bf16
-__device__ __forceinline__ void restore16(uint4 c, float s, uint4 (&out)[2])
+__device__ __forceinline__ void restore16(i32x4 c, float s, i32x4 (&out)[2])
 {
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-    uint32_t o[8];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[q], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[q], true);
-        o[2 * q] = pack_bf16(lo[0] * s, lo[1] * s);
-        o[2 * q + 1] = pack_bf16(hi[0] * s, hi[1] * s);
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(c[q], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(c[q], true);
+        out[q >> 1][2 * (q & 1)] = (int)pack_bf16(lo[0] * s, lo[1] * s);
+        out[q >> 1][2 * (q & 1) + 1] = (int)pack_bf16(hi[0] * s, hi[1] * s);
     }
-    out[0] = make_uint4(o[0], o[1], o[2], o[3]);
-    out[1] = make_uint4(o[4], o[5], o[6], o[7]);
 }
 }  // namespace
+
+// rows x cols codes (fragment order of k_linear.hip) and the scales of the rows -> B as described above.  A wave takes 32 rows and
+// 128 columns; the turn is ds_read_b64_tr_b16's.
+__global__ __launch_bounds__(256) void restore_turned_kernel(const uint8_t *__restrict__ codes, const float *__restrict__ scales, int rows, int cols, uint8_t *__restrict__ B)
+{
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * 8192];
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+    const int spans = cols / 128, groups = (rows + 31) / 32;
+    const long at = (long)blockIdx.x * 4 + wave;
+    if (at >= (long)groups * spans) return;          // the whole wave leaves; nothing below synchronises across waves
+    const int grp = (int)(at / spans), span = (int)(at - (long)grp * spans), R = min(32, rows - 32 * grp), r = lane & 31;
+    uint8_t *const tile = smem + wave * 8192;
+    const uint8_t *const from = codes + (size_t)grp * 32 * cols + (size_t)span * 128 * R;
+    const float scale = r < R ? scales[32 * grp + r] : 0.f;
+    i32x4 c[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {                    // piece (slice, run): 16 columns of row r
+        const int slice = x >> 1, run = (x & 1) * 2 + (lane >> 5);
+        c[x] = r < R ? *(const i32x4 *)(from + slice * R * 64 + (run * R + r) * 16) : i32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        const int run = (x & 1) * 2 + (lane >> 5), col = 8 * (x >> 1) + 2 * (2 * (run & 1) + (run >> 1));      // run h * 2 + g holds the pieces of channels 32 g + 16 h
+        i32x4 v[2];
+        restore16(c[x], scale, v);
+        *(i32x4 *)(tile + r * 256 + (col ^ swizzle(r)) * 16) = v[0];
+        *(i32x4 *)(tile + r * 256 + ((col + 1) ^ swizzle(r)) * 16) = v[1];
+    }
+    wave_lds_sync();
+#pragma unroll
+    for (int x = 0; x < 4; ++x)                      // column groups; two slices of 16 k, 2 KB in a row
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+            *(bf16x8 *)(B + (((size_t)(span * 4 + x) * groups + grp) * 2 + t) * 1024 + lane * 16) = read_turned<128>(tile, 32 * x, t, lane);
+}
 
 // TURN: A(m,k) = A[k][m] (dW), else A[m][k] (dx); A is bf16 with `lda` elements to a row.  Workgroup tile 64 TM x 64 TN, four waves as
 // 2 x 2.  Split `s` of the summation covers k from s k_split on; with part != nullptr the tile goes there in fp32, [split][M][cols],
 // and, from the first tile of columns, the sums of A over k to part_db [split][M].
+//
+// Steps of 32 k, four stages in LDS, filled by copies three steps ahead.  A step has two parts of 16 k; the operands of a
+// part are read while the products of the one before run (two sets of registers).  The one barrier of a step stands before the products of its
+// second part, whose operands are in registers by then: everybody has read the stage, the next one is whole (its copies were asked for three
+// steps ago), and its first operands are read under those products.
+// With TM = TN = 4 a wave holds 256 accumulators and a CU one workgroup: a part takes 8 operands per 16 matrix instructions from
+// LDS, half of what its bandwidth allows (128 x 64 per wave: three quarters, with the writes all of it).
 template <int TM, int TN, bool TURN>
-__global__ __launch_bounds__(256) void linear_grad_kernel(const uint16_t *__restrict__ A, int lda, const uint8_t *__restrict__ codes,
-                                                          const float *__restrict__ scales, int M, int cols, int K, int k_split, int n_nt,
-                                                          int tiles, int total, uint16_t *__restrict__ C, float *__restrict__ part,
-                                                          float *__restrict__ part_db)
+__global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void linear_grad_kernel(const uint16_t *__restrict__ A, int lda, const uint8_t *__restrict__ B, int M, int cols,
+                                                          int K, int k_split, int n_nt, int tiles, int total, uint16_t *__restrict__ C,
+                                                          float *__restrict__ part, float *__restrict__ part_db)
 {
-    constexpr int BM = 64 * TM, BN = 64 * TN, kA = BM * kStepK * 2, kB = BN * kStepK * 2, kStage = kA + kB;
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * kStage];
+    constexpr int BM = 64 * TM, BN = 64 * TN, kA = BM * kStepK * 2, kB = BN * kStepK * 2, kStage = kA + kB, kStages = 4;
+    constexpr int kCopies = kStage / 4096, kCopiesA = kA / 4096;               // copies of 1 KB a wave makes in a step
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[kStages * kStage];
     const int item = (int)xcd_remap(blockIdx.x, total);
     if (item >= total) return;
     const int split = item / tiles, tile = item - split * tiles, mt = tile / n_nt, nt = tile - mt * n_nt;
     const int m0 = mt * BM, n0 = nt * BN, k0 = split * k_split, k1 = min(K, k0 + k_split);
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = (wave & 1) * 32 * TM, wn = (wave >> 1) * 32 * TN;
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
 
-    constexpr int kPb = TN / 2;                      // pieces of B a thread brings in a step
-    uint4 ra[TM], rb[kPb];
-    float rs[kPb];
-    auto load = [&](int k) {
+    // ---- copies: copy x of wave w brings bytes 1024 (w kCopiesA + x) .. of the stage's A, or of its B.  Rows and pieces past the end
+    // repeat the last ones: results of rows past M and columns past `cols` are not stored, and what of A lies past K is cleared (clear_tail).
+    uint32_t va[kCopiesA];
+    auto place = [&](int left) {                     // left: summation indices that are there, from the step's first on
 #pragma unroll
-        for (int x = 0; x < TM; ++x) {
-            const int id = x * 256 + tid;
-            ra[x] = make_uint4(0, 0, 0, 0);
+        for (int x = 0; x < kCopiesA; ++x) {
+            const int at = (wave * kCopiesA + x) * 1024 + lane * 16;
             if constexpr (TURN) {
-                const int kk = k + id / (BM / 8), m = m0 + id % (BM / 8) * 8;
-                if (kk < k1 && m < M) ra[x] = *(const uint4 *)(A + (size_t)kk * lda + m);
+                const int k = at / (2 * BM), c = (at % (2 * BM) / 16) ^ swizzle(k);
+                va[x] = (uint32_t)min(k, left - 1) * (uint32_t)lda * 2u + (uint32_t)min(m0 + 8 * c, M - 8) * 2u;
             } else {
-                const int m = m0 + id / 4, kk = k + id % 4 * 8;
-                if (kk < k1 && m < M) ra[x] = *(const uint4 *)(A + (size_t)m * lda + kk);
-            }
-        }
-        const int R = min(32, K - k);                // rows of the group of code rows that starts at k
-#pragma unroll
-        for (int x = 0; x < kPb; ++x) {
-            const int slice = x * 2 + (tid >> 7), run = (tid >> 5) & 3, r = tid & 31;
-            rb[x] = make_uint4(0, 0, 0, 0);
-            rs[x] = 0.f;
-            if (r < R && n0 + 64 * slice < cols) {
-                rb[x] = *(const uint4 *)(codes + (size_t)k * cols + (size_t)(n0 / 64 + slice) * R * 64 + (run * R + r) * 16);
-                rs[x] = scales[k + r];
+                const int m = at / 64, c = (at / 16 % 4) ^ (m >> 2 & 3);
+                va[x] = (uint32_t)min(m, M - 1 - m0) * (uint32_t)lda * 2u + (uint32_t)min(c, left / 8 - 1) * 16u;
             }
         }
     };
-    auto store = [&](uint8_t *st) {
+    const int groups = (K + 31) / 32;
+    const uint8_t *pb[kCopies - kCopiesA];           // two copies are a column group's step
 #pragma unroll
-        for (int x = 0; x < TM; ++x) {
-            const int id = x * 256 + tid;
-            if constexpr (TURN) {
-                const int kk = id / (BM / 8), c = id % (BM / 8);
-                *(uint4 *)(st + kk * (2 * BM) + (c ^ swizzle(kk)) * 16) = ra[x];
-            } else {
-                const int m = id / 4, c = id % 4;
-                *(uint4 *)(st + m * 64 + (c ^ ((m >> 2) & 3)) * 16) = ra[x];
-            }
-        }
+    for (int x = 0; x < kCopies - kCopiesA; ++x) {
+        const int id = wave * (kCopies - kCopiesA) + x;
+        pb[x] = B + ((size_t)min(n0 / 32 + (id >> 1), cols / 32 - 1) * groups * 2 + (id & 1)) * 1024;
+    }
+    auto copy = [&](int k, int stage) {
+        if (K - k < kStepK) place(K - k);            // the last step of all
+        const uint8_t *const base = (const uint8_t *)A + (TURN ? (size_t)k * lda * 2 : (size_t)m0 * lda * 2 + (size_t)k * 2);
+        const uint32_t to = lds_base + stage * kStage;
 #pragma unroll
-        for (int x = 0; x < kPb; ++x) {
-            const int slice = x * 2 + (tid >> 7), run = (tid >> 5) & 3, r = tid & 31;
-            const int c = 8 * slice + 2 * (2 * (run & 1) + (run >> 1));        // run h * 2 + g holds the pieces of channels 32 g + 16 h
-            uint4 v[2];
-            restore16(rb[x], rs[x], v);
-            uint8_t *const row = st + kA + r * (2 * BN);
-            *(uint4 *)(row + (c ^ swizzle(r)) * 16) = v[0];
-            *(uint4 *)(row + ((c + 1) ^ swizzle(r)) * 16) = v[1];
+        for (int x = 0; x < kCopiesA; ++x) copy_1k_to_lds(base, va[x], to + (wave * kCopiesA + x) * 1024);
+#pragma unroll
+        for (int x = 0; x < kCopies - kCopiesA; ++x) copy_1k_to_lds(pb[x] + (size_t)k * 64, lane * 16, to + kA + (wave * (kCopies - kCopiesA) + x) * 1024);
+    };
+    auto clear_tail = [&](int left, int stage) {     // whole pieces (dx: K is a multiple of 8) or rows (dW)
+        for (int at = tid * 16; at < kA; at += 4096) {
+            const int k = TURN ? at / (2 * BM) : 8 * ((at / 16 % 4) ^ (at / 256 & 3));
+            if (k >= left) *(i32x4 *)(smem + stage * kStage + at) = i32x4{0, 0, 0, 0};
         }
     };
 
@@ -138,43 +169,68 @@ __global__ __launch_bounds__(256) void linear_grad_kernel(const uint16_t *__rest
     for (int a = 0; a < TM; ++a) sums[a] = 0.f;
     const bool summing = TURN && part_db && nt == 0 && wn == 0;
 
-    const int steps = (k1 - k0 + kStepK - 1) / kStepK;
-    load(k0);
-    store(smem);
-    __syncthreads();
-    for (int s = 0; s < steps; ++s) {
-        const uint8_t *const st = smem + (s & 1) * kStage;
-        if (s + 1 < steps) load(k0 + (s + 1) * kStepK);
+    bf16x8 af[2][TM], bf[2][TN];
+    auto read = [&](int set, int stage, int t) {
+        const uint8_t *const st = smem + stage * kStage;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            bf16x8 af[TM], bf[TN];
+        for (int b = 0; b < TN; ++b) bf[set][b] = *(const bf16x8 *)(st + kA + ((wn / 32 + b) * 2 + t) * 1024 + lane * 16);
 #pragma unroll
-            for (int a = 0; a < TM; ++a) {
-                if constexpr (TURN) af[a] = read_turned<BM>(st, wm + 32 * a, t, lane);
-                else {
-                    const int m = wm + 32 * a + l32;
-                    af[a] = *(const bf16x8 *)(st + m * 64 + ((2 * t + g) ^ ((m >> 2) & 3)) * 16);
-                }
-            }
-#pragma unroll
-            for (int b = 0; b < TN; ++b) bf[b] = read_turned<BN>(st + kA, wn + 32 * b, t, lane);
-#pragma unroll
-            for (int b = 0; b < TN; ++b)
-#pragma unroll
-                for (int a = 0; a < TM; ++a) acc[b][a] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[b], af[a], acc[b][a], 0, 0, 0);
-            if (summing) {
-#pragma unroll
-                for (int a = 0; a < TM; ++a) {
-                    const uint4 u = __builtin_bit_cast(uint4, af[a]);
-                    sums[a] = dot2_bf16(u.x, 0x3F803F80u, dot2_bf16(u.y, 0x3F803F80u, dot2_bf16(u.z, 0x3F803F80u, dot2_bf16(u.w, 0x3F803F80u, sums[a]))));
-                }
+        for (int a = 0; a < TM; ++a) {
+            if constexpr (TURN) af[set][a] = read_turned<BM>(st, wm + 32 * a, t, lane);
+            else {
+                const int m = wm + 32 * a + l32;
+                af[set][a] = *(const bf16x8 *)(st + m * 64 + ((2 * t + g) ^ (m >> 2 & 3)) * 16);
             }
         }
-        if (s + 1 < steps) store(smem + ((s + 1) & 1) * kStage);
-        __syncthreads();
+    };
+    auto multiply = [&](int set) {
+#pragma unroll
+        for (int b = 0; b < TN; ++b)
+#pragma unroll
+            for (int a = 0; a < TM; ++a) acc[b][a] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[set][b], af[set][a], acc[b][a], 0, 0, 0);
+        if (summing) {
+#pragma unroll
+            for (int a = 0; a < TM; ++a) {
+                const uint4 u = __builtin_bit_cast(uint4, af[set][a]);
+                sums[a] = dot2_bf16(u.x, 0x3F803F80u, dot2_bf16(u.y, 0x3F803F80u, dot2_bf16(u.z, 0x3F803F80u, dot2_bf16(u.w, 0x3F803F80u, sums[a]))));
+            }
+        }
+    };
+    // the stage of step k is whole and everybody is done with the one before it; `ahead`: later steps whose copies may still be under way
+    auto change = [&](int k, int stage, int ahead) {
+        if (ahead >= 2)      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kCopies) : "memory");
+        else if (ahead == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kCopies) : "memory");
+        else                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        lds_barrier();
+        if (K - k < kStepK) {
+            clear_tail(K - k, stage);
+            lds_barrier();
+        }
+    };
+
+    place(kStepK);
+    const int steps = (k1 - k0 + kStepK - 1) / kStepK;
+    for (int s = 0; s < min(steps, 3); ++s) copy(k0 + s * kStepK, s);
+    change(k0, 0, min(steps - 1, 2));
+    read(0, 0, 0);
+    for (int s = 0; s < steps; ++s) {
+        const int k = k0 + s * kStepK;
+        if (s + 3 < steps) copy(k + 3 * kStepK, (s + 3) & 3);
+        read(1, s & 3, 1);
+        multiply(0);
+        if (s + 1 < steps) {
+            change(k + kStepK, (s + 1) & 3, min(steps - s - 2, 2));
+            read(0, (s + 1) & 3, 0);
+        }
+        multiply(1);
     }
 
     // register 4q + r of acc[b][a], lane (l32, g): n = 32 b + 8 q + 4 g + r, m = 32 a + l32
+    auto swap32 = [](uint32_t &lo, uint32_t &hi) {                               // upper lanes of lo <-> lower lanes of hi
+        const auto r = __builtin_amdgcn_permlane32_swap(lo, hi, false, false);
+        lo = r[0];
+        hi = r[1];
+    };
 #pragma unroll
     for (int a = 0; a < TM; ++a) {
         const int m = m0 + wm + 32 * a + l32;
@@ -183,15 +239,26 @@ __global__ __launch_bounds__(256) void linear_grad_kernel(const uint16_t *__rest
             if (g == 0 && m < M) part_db[(size_t)split * M + m] = v;
         }
 #pragma unroll
-        for (int b = 0; b < TN; ++b)
+        for (int b = 0; b < TN; ++b) {
+            const f32x16 &v = acc[b][a];
+            if (part) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int n = n0 + wn + 32 * b + 8 * q + 4 * g;
-                if (m >= M || n >= cols) continue;
-                const float v[4] = {acc[b][a][4 * q], acc[b][a][4 * q + 1], acc[b][a][4 * q + 2], acc[b][a][4 * q + 3]};
-                if (part) *(float4 *)(part + ((size_t)split * M + m) * cols + n) = make_float4(v[0], v[1], v[2], v[3]);
-                else *(uint2 *)(C + (size_t)m * cols + n) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+                for (int q = 0; q < 4; ++q) {
+                    const int n = n0 + wn + 32 * b + 8 * q + 4 * g;
+                    if (m < M && n < cols) *(float4 *)(part + ((size_t)split * M + m) * cols + n) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; q += 2) {
+                    uint32_t x0 = pack_bf16(v[4 * q], v[4 * q + 1]), y0 = pack_bf16(v[4 * q + 2], v[4 * q + 3]);
+                    uint32_t x1 = pack_bf16(v[4 * q + 4], v[4 * q + 5]), y1 = pack_bf16(v[4 * q + 6], v[4 * q + 7]);
+                    swap32(x0, x1);
+                    swap32(y0, y1);
+                    const int n = n0 + wn + 32 * b + 8 * q + 8 * g;
+                    if (m < M && n < cols) *(uint4 *)(C + (size_t)m * cols + n) = make_uint4(x0, y0, x1, y1);
+                }
             }
+        }
     }
 }
 
@@ -218,53 +285,71 @@ __global__ __launch_bounds__(256) void restore_rows_kernel(const uint8_t *__rest
     const long grp = at / (32 * pieces);
     const int R = (int)min(32L, rows - 32 * grp), in = (int)(at - grp * 32 * pieces);
     const int slice = in / (4 * R), rest = in - slice * 4 * R, run = rest / R, r = rest - run * R;
-    uint4 v[2];
-    restore16(*(const uint4 *)(codes + at * 16), scales[32 * grp + r], v);
+    i32x4 v[2];
+    restore16(*(const i32x4 *)(codes + at * 16), scales[32 * grp + r], v);
     uint16_t *const x = X + (32 * grp + r) * cols + 64 * slice + 16 * (2 * (run & 1) + (run >> 1));
-    *(uint4 *)x = v[0];
-    *(uint4 *)(x + 8) = v[1];
+    *(i32x4 *)x = v[0];
+    *(i32x4 *)(x + 8) = v[1];
 }
 
 namespace {
-constexpr int kGradTile = 128;                       // rows and columns of a workgroup's tile
-
-template <bool TURN>
-hipError_t launch_grad(const void *A, int lda, const void *codes, const float *scales, int M, int cols, int K, int splits, void *C, float *part,
-                       float *part_db, hipStream_t st)
+template <int T, bool TURN>
+hipError_t launch_grad(const void *A, int lda, const void *B, int M, int cols, int K, int splits, void *C, float *part, float *part_db, hipStream_t st)
 {
-    const int n_mt = (M + kGradTile - 1) / kGradTile, n_nt = (cols + kGradTile - 1) / kGradTile;
+    const int n_mt = (M + 64 * T - 1) / (64 * T), n_nt = (cols + 64 * T - 1) / (64 * T);
     const long tiles = (long)n_mt * n_nt, total = tiles * splits;
     if (total > 0x7FFFFFF0L) return hipErrorInvalidValue;
     const int steps = (K + kStepK - 1) / kStepK, k_split = (steps + splits - 1) / splits * kStepK;
-    linear_grad_kernel<2, 2, TURN><<<(unsigned)xcd_grid(total), 256, 0, st>>>((const uint16_t *)A, lda, (const uint8_t *)codes, scales, M, cols, K, k_split,
+    linear_grad_kernel<T, T, TURN><<<(unsigned)xcd_grid(total), 256, 0, st>>>((const uint16_t *)A, lda, (const uint8_t *)B, M, cols, K, k_split,
                                                                               n_nt, (int)tiles, (int)total, (uint16_t *)C, part, part_db);
     return hipGetLastError();
 }
-}  // namespace
-
-// Splits of the sum over the tokens: enough workgroups for the chip where dW has few tiles, each with at least eight steps.
-int linear_grad_splits(int N, int d_in, int d_out)
+hipError_t launch_restore_turned(const void *codes, const float *scales, int rows, int cols, void *B, hipStream_t st)
 {
-    const long tiles = (long)((d_out + kGradTile - 1) / kGradTile) * ((d_in + kGradTile - 1) / kGradTile);
+    const long waves = (long)((rows + 31) / 32) * (cols / 128);
+    restore_turned_kernel<<<(unsigned)((waves + 3) / 4), 256, 0, st>>>((const uint8_t *)codes, scales, rows, cols, (uint8_t *)B);
+    return hipGetLastError();
+}
+long tiles_of(int M, int cols, int size) { return (long)((M + size - 1) / size) * ((cols + size - 1) / size); }
+
+// Tiles and splits of dW: enough workgroups for the chip, each split with at least eight steps, none without steps.
+struct GradPlan { int wide, splits; };
+GradPlan dw_plan(int N, int d_in, int d_out)
+{
     const int steps = (N + kStepK - 1) / kStepK;
-    long s = 768 / tiles;
+    GradPlan p;
+    p.wide = tiles_of(d_out, d_in, 256) * (steps / 8) >= 256;
+    long s = p.wide ? 256 / tiles_of(d_out, d_in, 256) : 512 / tiles_of(d_out, d_in, 128);
     s = s > steps / 8 ? steps / 8 : s;
     s = s < 1 ? 1 : s;
-    return steps ? (int)((steps + (steps + s - 1) / s - 1) / ((steps + s - 1) / s)) : 0;     // no split without steps
+    p.splits = steps ? (int)((steps + (steps + s - 1) / s - 1) / ((steps + s - 1) / s)) : 0;
+    return p;
+}
+}  // namespace
+
+int linear_grad_splits(int N, int d_in, int d_out) { return dw_plan(N, d_in, d_out).splits; }
+
+size_t linear_grad_turned_bytes(int rows, int cols) { return (size_t)((rows + 31) / 32) * 32 * cols * 2; }
+
+hipError_t launch_linear_dx(const void *dy, const void *w8, const float *sw, int N, int d_in, int d_out, void *dx, void *turned, hipStream_t st)
+{
+    const hipError_t e = launch_restore_turned(w8, sw, d_out, d_in, turned, st);
+    if (e != hipSuccess) return e;
+    if (tiles_of(N, d_in, 256) >= 160) return launch_grad<4, false>(dy, d_out, turned, N, d_in, d_out, 1, dx, nullptr, nullptr, st);
+    return launch_grad<2, false>(dy, d_out, turned, N, d_in, d_out, 1, dx, nullptr, nullptr, st);
 }
 
-hipError_t launch_linear_dx(const void *dy, const void *w8, const float *sw, int N, int d_in, int d_out, void *dx, hipStream_t st)
+hipError_t launch_linear_dw(const void *dy, const void *x8, const float *sx, int N, int d_in, int d_out, void *dW, void *db, void *turned, float *part, hipStream_t st)
 {
-    return launch_grad<false>(dy, d_out, w8, sw, N, d_in, d_out, 1, dx, nullptr, nullptr, st);
-}
-
-hipError_t launch_linear_dw(const void *dy, const void *x8, const float *sx, int N, int d_in, int d_out, void *dW, void *db, float *part, hipStream_t st)
-{
-    const int splits = linear_grad_splits(N, d_in, d_out);
+    const GradPlan p = dw_plan(N, d_in, d_out);
+    const int splits = p.splits;
     const long count = (long)d_out * d_in;
     float *const part_db = part + (size_t)splits * count;
     if (splits) {
-        const hipError_t e = launch_grad<true>(dy, d_out, x8, sx, d_out, d_in, N, splits, nullptr, part, db ? part_db : nullptr, st);
+        hipError_t e = launch_restore_turned(x8, sx, N, d_in, turned, st);
+        if (e != hipSuccess) return e;
+        e = p.wide ? launch_grad<4, true>(dy, d_out, turned, d_out, d_in, N, splits, nullptr, part, db ? part_db : nullptr, st)
+                   : launch_grad<2, true>(dy, d_out, turned, d_out, d_in, N, splits, nullptr, part, db ? part_db : nullptr, st);
         if (e != hipSuccess) return e;
     }
     linear_grad_reduce_kernel<<<(unsigned)((count / 4 + 255) / 256), 256, 0, st>>>(part, splits, count, (uint16_t *)dW);
