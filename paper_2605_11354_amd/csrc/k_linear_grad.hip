@@ -141,14 +141,16 @@ __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void linear_grad_kernel(const
         const int id = wave * (kCopies - kCopiesA) + x;
         pb[x] = B + ((size_t)min(n0 / 32 + (id >> 1), cols / 32 - 1) * groups * 2 + (id & 1)) * 1024;
     }
-    auto copy = [&](int k, int stage) {
+    const uint8_t *base;                             // of the step that is copied next
+    uint32_t to;
+    auto aim = [&](int k, int stage) {
         if (K - k < kStepK) place(K - k);            // the last step of all
-        const uint8_t *const base = (const uint8_t *)A + (TURN ? (size_t)k * lda * 2 : (size_t)m0 * lda * 2 + (size_t)k * 2);
-        const uint32_t to = lds_base + stage * kStage;
-#pragma unroll
-        for (int x = 0; x < kCopiesA; ++x) copy_1k_to_lds(base, va[x], to + (wave * kCopiesA + x) * 1024);
-#pragma unroll
-        for (int x = 0; x < kCopies - kCopiesA; ++x) copy_1k_to_lds(pb[x] + (size_t)k * 64, lane * 16, to + kA + (wave * (kCopies - kCopiesA) + x) * 1024);
+        base = (const uint8_t *)A + (TURN ? (size_t)k * lda * 2 : (size_t)m0 * lda * 2 + (size_t)k * 2);
+        to = lds_base + stage * kStage;
+    };
+    auto copy_one = [&](int k, int x) {
+        if (x < kCopiesA) copy_1k_to_lds(base, va[x], to + (wave * kCopiesA + x) * 1024);
+        else copy_1k_to_lds(pb[x - kCopiesA] + (size_t)k * 64, lane * 16, to + kA + (wave * (kCopies - kCopiesA) + x - kCopiesA) * 1024);
     };
     auto clear_tail = [&](int left, int stage) {     // whole pieces (dx: K is a multiple of 8) or rows (dW)
         for (int at = tid * 16; at < kA; at += 4096) {
@@ -168,26 +170,29 @@ __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void linear_grad_kernel(const
 #pragma unroll
     for (int a = 0; a < TM; ++a) sums[a] = 0.f;
     const bool summing = TURN && part_db && nt == 0 && wn == 0;
+    const int steps = (k1 - k0 + kStepK - 1) / kStepK;                           // at least one
 
     bf16x8 af[2][TM], bf[2][TN];
-    auto read = [&](int set, int stage, int t) {
+    auto read_one = [&](int set, int stage, int t, int x) {                      // operand x: TN of B, then TM of A
         const uint8_t *const st = smem + stage * kStage;
-#pragma unroll
-        for (int b = 0; b < TN; ++b) bf[set][b] = *(const bf16x8 *)(st + kA + ((wn / 32 + b) * 2 + t) * 1024 + lane * 16);
-#pragma unroll
-        for (int a = 0; a < TM; ++a) {
-            if constexpr (TURN) af[set][a] = read_turned<BM>(st, wm + 32 * a, t, lane);
-            else {
-                const int m = wm + 32 * a + l32;
-                af[set][a] = *(const bf16x8 *)(st + m * 64 + ((2 * t + g) ^ (m >> 2 & 3)) * 16);
-            }
+        if (x < TN) bf[set][x] = *(const bf16x8 *)(st + kA + ((wn / 32 + x) * 2 + t) * 1024 + lane * 16);
+        else if constexpr (TURN) af[set][x - TN] = read_turned<BM>(st, wm + 32 * (x - TN), t, lane);
+        else {
+            const int m = wm + 32 * (x - TN) + l32;
+            af[set][x - TN] = *(const bf16x8 *)(st + m * 64 + ((2 * t + g) ^ (m >> 2 & 3)) * 16);
         }
     };
-    auto multiply = [&](int set) {
+    // the products of a part; what `between` does goes behind each of them, since a wave is alone on its SIMD: everything that is not
+    // issued in the 28 cycles that a matrix instruction goes on by itself leaves the matrix unit idle
+    auto multiply = [&](int set, auto between) {
 #pragma unroll
-        for (int b = 0; b < TN; ++b)
-#pragma unroll
-            for (int a = 0; a < TM; ++a) acc[b][a] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[set][b], af[set][a], acc[b][a], 0, 0, 0);
+        for (int i = 0; i < TM * TN; ++i) {
+            const int b = i / TM, a = i % TM;
+            acc[b][a] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[set][b], af[set][a], acc[b][a], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            between(i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         if (summing) {
 #pragma unroll
             for (int a = 0; a < TM; ++a) {
@@ -196,34 +201,61 @@ __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void linear_grad_kernel(const
             }
         }
     };
-    // the stage of step k is whole and everybody is done with the one before it; `ahead`: later steps whose copies may still be under way
-    auto change = [&](int k, int stage, int ahead) {
-        if (ahead >= 2)      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kCopies) : "memory");
-        else if (ahead == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kCopies) : "memory");
-        else                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // the next stage is whole and everybody is done with the one before it; AHEAD: later steps whose copies may still be under way
+    auto change = [&](auto ahead) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(ahead)::value * kCopies) : "memory");
         lds_barrier();
-        if (K - k < kStepK) {
-            clear_tail(K - k, stage);
+    };
+    auto change_to_last = [&](int stage) {           // and what of it lies past K is cleared
+        const int left = K - (k0 + (steps - 1) * kStepK);
+        if (left < kStepK) {
+            clear_tail(left, stage);
             lds_barrier();
         }
     };
+    constexpr int kOperands = TM + TN, kEvery = TM * TN / kCopies > 0 ? TM * TN / kCopies : 1;
+    auto step = [&](int s, auto copies, auto ahead, auto last) {
+        constexpr bool kCopy = decltype(copies)::value, kLast = decltype(last)::value;
+        const int k3 = k0 + (s + 3) * kStepK;
+        if constexpr (kCopy) aim(k3, (s + 3) & 3);
+        multiply(0, [&](int i) {
+            if (i < kOperands) read_one(1, s & 3, 1, i);
+            if constexpr (kCopy)
+                if (i % kEvery == 0 && i / kEvery < kCopies) copy_one(k3, i / kEvery);
+        });
+        if constexpr (!kLast) {
+            change(ahead);
+            if constexpr (decltype(ahead)::value == 0) change_to_last((s + 1) & 3);
+        }
+        multiply(1, [&](int i) {
+            if constexpr (!kLast)
+                if (i < kOperands) read_one(0, (s + 1) & 3, 0, i);
+        });
+    };
+    static_assert(kOperands <= TM * TN && kCopies * kEvery <= TM * TN, "a part has room for its reads and copies");
+    using Ahead0 = std::integral_constant<int, 0>;
+    using Ahead1 = std::integral_constant<int, 1>;
+    using Ahead2 = std::integral_constant<int, 2>;
+    using Yes = std::true_type;
+    using No = std::false_type;
 
     place(kStepK);
-    const int steps = (k1 - k0 + kStepK - 1) / kStepK;
-    for (int s = 0; s < min(steps, 3); ++s) copy(k0 + s * kStepK, s);
-    change(k0, 0, min(steps - 1, 2));
-    read(0, 0, 0);
-    for (int s = 0; s < steps; ++s) {
-        const int k = k0 + s * kStepK;
-        if (s + 3 < steps) copy(k + 3 * kStepK, (s + 3) & 3);
-        read(1, s & 3, 1);
-        multiply(0);
-        if (s + 1 < steps) {
-            change(k + kStepK, (s + 1) & 3, min(steps - s - 2, 2));
-            read(0, (s + 1) & 3, 0);
-        }
-        multiply(1);
+    for (int s = 0; s < min(steps, 3); ++s) {
+        aim(k0 + s * kStepK, s);
+#pragma unroll
+        for (int x = 0; x < kCopies; ++x) copy_one(k0 + s * kStepK, x);
     }
+    if (steps > 2) change(Ahead2{});
+    else if (steps == 2) change(Ahead1{});
+    else change(Ahead0{});
+    if (steps == 1) change_to_last(0);
+#pragma unroll
+    for (int x = 0; x < kOperands; ++x) read_one(0, 0, 0, x);
+    int s = 0;
+    for (; s + 3 < steps; ++s) step(s, Yes{}, Ahead2{}, No{});
+    if (s + 2 < steps) step(s++, No{}, Ahead1{}, No{});
+    if (s + 1 < steps) step(s++, No{}, Ahead0{}, No{});
+    step(s, No{}, Ahead0{}, Yes{});
 
     // register 4q + r of acc[b][a], lane (l32, g): n = 32 b + 8 q + 4 g + r, m = 32 a + l32
     auto swap32 = [](uint32_t &lo, uint32_t &hi) {                               // upper lanes of lo <-> lower lanes of hi
