@@ -10,19 +10,20 @@
 // index, so it cannot wait for the epilogue.  Rounding code x scale to bf16 is off by at most 2^-8 of it, as the rounding of x to bf16
 // was in the first place; products are exact in the fp32 accumulators.
 //
-// B is restored once, by restore_turned_kernel, into the order in which the matrix unit's operands are read: column groups of 32, of
+// B is restored once, by grad_operands_kernel, into the order in which the matrix unit's operands are read: column groups of 32, of
 // a group 16 k after 16 k, 1 KB each, lane l's 16 bytes (column l % 32, k = 8 (l / 32) ..) one after the other; k past the end are
 // zeros up to a multiple of 32.  (Converted on the way to LDS instead, every tile of rows converts it again: four vector instructions
 // for each matrix instruction, 540 us instead of 30 for the restoring and what the products then take.)
 #include "sla_common.hpp"
 #include "sla_kernels.hpp"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace sla {
 
 namespace {
-constexpr int kStepK = 32;                           // summation indices of a step
+constexpr int kStepK = 32, kStages = 4;              // summation indices of a step; steps in LDS
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 
 // Tiles that lie [k][column] in LDS: a row is 2 columns bytes, its 16-byte piece c at position c ^ swizzle(k).  Four
@@ -57,28 +58,15 @@ __device__ __forceinline__ void restore16(i32x4 c, float s, i32x4 (&out)[2])
 }
 }  // namespace
 
-// rows x cols codes (fragment order of k_linear.hip) and the scales of the rows -> B as described above.  A wave takes 32 rows and
-// 128 columns; the turn is ds_read_b64_tr_b16's.
-__global__ __launch_bounds__(256) void restore_turned_kernel(const uint8_t *__restrict__ codes, const float *__restrict__ scales, int rows, int cols, uint8_t *__restrict__ B)
+// Codes of a 32 x 128 tile, lane l's four pieces (columns 16 (x / 2 * 4 + 2 (run % 2) + run / 2) .. of row l % 32, run = x % 2 * 2 + l / 32:
+// the order of k_linear.hip), times the scale of the lane's row -> B as described above: column groups 4 span .. + 3, row group grp.
+// `tile`: 8 KB of the wave's own LDS; the turn is ds_read_b64_tr_b16's.
+__device__ __forceinline__ void turn_tile(const i32x4 (&c)[4], float scale, uint8_t *tile, int lane, int span, int grp, int groups, uint8_t *B)
 {
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * 8192];
-    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
-    const int spans = cols / 128, groups = (rows + 31) / 32;
-    const long at = (long)blockIdx.x * 4 + wave;
-    if (at >= (long)groups * spans) return;          // the whole wave leaves; nothing below synchronises across waves
-    const int grp = (int)(at / spans), span = (int)(at - (long)grp * spans), R = min(32, rows - 32 * grp), r = lane & 31;
-    uint8_t *const tile = smem + wave * 8192;
-    const uint8_t *const from = codes + (size_t)grp * 32 * cols + (size_t)span * 128 * R;
-    const float scale = r < R ? scales[32 * grp + r] : 0.f;
-    i32x4 c[4];
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {                    // piece (slice, run): 16 columns of row r
-        const int slice = x >> 1, run = (x & 1) * 2 + (lane >> 5);
-        c[x] = r < R ? *(const i32x4 *)(from + slice * R * 64 + (run * R + r) * 16) : i32x4{0, 0, 0, 0};
-    }
+    const int r = lane & 31;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-        const int run = (x & 1) * 2 + (lane >> 5), col = 8 * (x >> 1) + 2 * (2 * (run & 1) + (run >> 1));      // run h * 2 + g holds the pieces of channels 32 g + 16 h
+        const int run = (x & 1) * 2 + (lane >> 5), col = 8 * (x >> 1) + 2 * (2 * (run & 1) + (run >> 1));
         i32x4 v[2];
         restore16(c[x], scale, v);
         *(i32x4 *)(tile + r * 256 + (col ^ swizzle(r)) * 16) = v[0];
@@ -92,9 +80,79 @@ __global__ __launch_bounds__(256) void restore_turned_kernel(const uint8_t *__re
             *(bf16x8 *)(B + (((size_t)(span * 4 + x) * groups + grp) * 2 + t) * 1024 + lane * 16) = read_turned<128>(tile, 32 * x, t, lane);
 }
 
-// TURN: A(m,k) = A[k][m] (dW), else A[m][k] (dx); A is bf16 with `lda` elements to a row.  Workgroup tile 64 TM x 64 TN, four waves as
-// 2 x 2.  Split `s` of the summation covers k from s k_split on; with part != nullptr the tile goes there in fp32, [split][M][cols],
-// and, from the first tile of columns, the sums of A over k to part_db [split][M].
+// Both products' B in one launch.  The first w_blocks workgroups quantise W (bf16 [d_out, cols]) as the layer's forward does and turn
+// the numbers at once: a workgroup takes 32 rows and 512 columns, for which it needs the maxima of the whole rows.  The others turn the
+// kept codes of x: 32 rows and 128 columns a wave.
+__global__ __launch_bounds__(256) void grad_operands_kernel(const uint16_t *__restrict__ W, int d_out, uint8_t *__restrict__ Bw, unsigned w_blocks,
+                                                            const uint8_t *__restrict__ codes, const float *__restrict__ scales, int rows,
+                                                            uint8_t *__restrict__ Bx, int cols)
+{
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * 8192];
+    __shared__ float red[4][32];
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, r = lane & 31;
+    const int spans = cols / 128;
+    i32x4 c[4];
+    if (blockIdx.x < w_blocks) {
+        const int parts = (spans + 3) / 4, grp = (int)(blockIdx.x / (unsigned)parts), span = (int)(blockIdx.x - grp * (unsigned)parts) * 4 + wave;
+        const int R = min(32, d_out - 32 * grp);
+        const uint16_t *const from = W + (size_t)32 * grp * cols;
+        float top[4] = {0.f, 0.f, 0.f, 0.f};         // of rows lane / 8 + 8 i, over 64 columns at a time
+        for (int s = wave; s < cols / 64; s += 4)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint4 u = *(const uint4 *)(from + (size_t)min((lane >> 3) + 8 * i, R - 1) * cols + 64 * s + 8 * (lane & 7));
+                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) top[i] = fmaxf(top[i], fmaxf(fabsf(bf16_lo(w[q])), fabsf(bf16_hi(w[q]))));
+            }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int x = 1; x < 8; x <<= 1) top[i] = fmaxf(top[i], __shfl_xor(top[i], x, 64));
+            if ((lane & 7) == 0) red[wave][(lane >> 3) + 8 * i] = top[i];
+        }
+        __syncthreads();
+        if (span >= spans) return;                   // nothing below synchronises across waves
+        const float scale = fmaxf(fmaxf(fmaxf(red[0][r], red[1][r]), fmaxf(red[2][r], red[3][r])), 1e-8f) / 448.0f;
+        const BlockDivisor divide(scale);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int run = (x & 1) * 2 + (lane >> 5), col = 16 * (4 * (x >> 1) + 2 * (run & 1) + (run >> 1));
+            const uint16_t *const at = from + (size_t)min(r, R - 1) * cols + 128 * span + col;
+            const uint4 u = *(const uint4 *)at, v = *(const uint4 *)(at + 8);
+            const uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+            c[x] = __builtin_bit_cast(i32x4, quantise16(w, divide));
+        }
+        // rows that are not there: zeros, of finite scale
+        if (r >= R) for (int x = 0; x < 4; ++x) c[x] = i32x4{0, 0, 0, 0};
+        turn_tile(c, r < R ? scale : 0.f, smem + wave * 8192, lane, span, grp, (d_out + 31) / 32, Bw);
+    } else {
+        const int groups = (rows + 31) / 32;
+        const long at = (long)(blockIdx.x - w_blocks) * 4 + wave;
+        if (at >= (long)groups * spans) return;
+        const int grp = (int)(at / spans), span = (int)(at - (long)grp * spans), R = min(32, rows - 32 * grp);
+        const uint8_t *const from = codes + (size_t)grp * 32 * cols + (size_t)span * 128 * R;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int run = (x & 1) * 2 + (lane >> 5);
+            c[x] = r < R ? *(const i32x4 *)(from + (x >> 1) * R * 64 + (run * R + r) * 16) : i32x4{0, 0, 0, 0};
+        }
+        turn_tile(c, r < R ? scales[32 * grp + r] : 0.f, smem + wave * 8192, lane, span, grp, groups, Bx);
+    }
+}
+
+// One of the two products: C [M, cols] = A B, A bf16 with `lda` elements to a row, B as described above.  Split s of the summation covers k
+// from s k_split on.  With part != nullptr a tile goes there in fp32, [split][M][cols], else to C; db (dW only, may be NULL): the sums of A
+// over k, from the first tile of columns, to db or, split, to part_db [split][M].
+struct GradProduct {
+    const uint16_t *A;
+    const uint8_t *B;
+    int lda, M, cols, K, k_split, n_nt, tiles, total;
+    uint16_t *C, *db;
+    float *part, *part_db;
+};
+
+// TURN: A(m,k) = A[k][m] (dW), else A[m][k] (dx).  Workgroup tile 64 TM x 64 TN, four waves as 2 x 2.
 //
 // Steps of 32 k, four stages in LDS, filled by copies three steps ahead.  A step has two parts of 16 k; the operands of a
 // part are read while the products of the one before run (two sets of registers).  The one barrier of a step stands before the products of its
@@ -103,15 +161,14 @@ __global__ __launch_bounds__(256) void restore_turned_kernel(const uint8_t *__re
 // With TM = TN = 4 a wave holds 256 accumulators and a CU one workgroup: a part takes 8 operands per 16 matrix instructions from
 // LDS, half of what its bandwidth allows (128 x 64 per wave: three quarters, with the writes all of it).
 template <int TM, int TN, bool TURN>
-__global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void linear_grad_kernel(const uint16_t *__restrict__ A, int lda, const uint8_t *__restrict__ B, int M, int cols,
-                                                          int K, int k_split, int n_nt, int tiles, int total, uint16_t *__restrict__ C,
-                                                          float *__restrict__ part, float *__restrict__ part_db)
+__device__ __forceinline__ void grad_tile(const GradProduct &p, int item, uint8_t *smem)
 {
-    constexpr int BM = 64 * TM, BN = 64 * TN, kA = BM * kStepK * 2, kB = BN * kStepK * 2, kStage = kA + kB, kStages = 4;
+    constexpr int BM = 64 * TM, BN = 64 * TN, kA = BM * kStepK * 2, kB = BN * kStepK * 2, kStage = kA + kB;
     constexpr int kCopies = kStage / 4096, kCopiesA = kA / 4096;               // copies of 1 KB a wave makes in a step
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[kStages * kStage];
-    const int item = (int)xcd_remap(blockIdx.x, total);
-    if (item >= total) return;
+    const uint16_t *const A = p.A;
+    const uint8_t *const B = p.B;
+    const int lda = p.lda, M = p.M, cols = p.cols, K = p.K, tiles = p.tiles, n_nt = p.n_nt, k_split = p.k_split;
+    float *const part = p.part;
     const int split = item / tiles, tile = item - split * tiles, mt = tile / n_nt, nt = tile - mt * n_nt;
     const int m0 = mt * BM, n0 = nt * BN, k0 = split * k_split, k1 = min(K, k0 + k_split);
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
@@ -169,7 +226,7 @@ __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void linear_grad_kernel(const
     float sums[TM];
 #pragma unroll
     for (int a = 0; a < TM; ++a) sums[a] = 0.f;
-    const bool summing = TURN && part_db && nt == 0 && wn == 0;
+    const bool summing = TURN && p.db && nt == 0 && wn == 0;
     const int steps = (k1 - k0 + kStepK - 1) / kStepK;                           // at least one
 
     bf16x8 af[2][TM], bf[2][TN];
@@ -268,7 +325,10 @@ __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void linear_grad_kernel(const
         const int m = m0 + wm + 32 * a + l32;
         if (summing) {
             const float v = sums[a] + xchg32(sums[a]);
-            if (g == 0 && m < M) part_db[(size_t)split * M + m] = v;
+            if (g == 0 && m < M) {
+                if (part) p.part_db[(size_t)split * M + m] = v;
+                else p.db[m] = (uint16_t)pack_bf16(v, v);
+            }
         }
 #pragma unroll
         for (int b = 0; b < TN; ++b) {
@@ -287,25 +347,49 @@ __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void linear_grad_kernel(const
                     swap32(x0, x1);
                     swap32(y0, y1);
                     const int n = n0 + wn + 32 * b + 8 * q + 8 * g;
-                    if (m < M && n < cols) *(uint4 *)(C + (size_t)m * cols + n) = make_uint4(x0, y0, x1, y1);
+                    if (m < M && n < cols) *(uint4 *)(p.C + (size_t)m * cols + n) = make_uint4(x0, y0, x1, y1);
                 }
             }
         }
     }
 }
 
-// out[i] = bf16(sum of the splits' partials, in order); count values (a multiple of 8)
-__global__ __launch_bounds__(256) void linear_grad_reduce_kernel(const float *__restrict__ part, int splits, long count, uint16_t *__restrict__ out)
+// The first grid_w workgroups (a multiple of 8) take the tiles of dW, the others those of dx: one launch, and the longer sums first.
+template <int T>
+__global__ __launch_bounds__(256, T == 4 ? 1 : 2) void linear_grad_kernel(GradProduct w, GradProduct x, unsigned grid_w)
 {
-    const long i = ((long)blockIdx.x * 256 + threadIdx.x) * 4;
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[kStages * 64 * (T + T) * kStepK * 2];
+    if (blockIdx.x < grid_w) {
+        const int item = (int)xcd_remap(blockIdx.x, w.total);
+        if (item < w.total) grad_tile<T, T, true>(w, item, smem);
+    } else {
+        const int item = (int)xcd_remap(blockIdx.x - grid_w, x.total);
+        if (item < x.total) grad_tile<T, T, false>(x, item, smem);
+    }
+}
+
+// out[i] = bf16(sum of the splits' partials, in order), for up to three outputs; counts are multiples of 8
+struct GradSums {
+    const float *part[3];
+    uint16_t *out[3];
+    long count[3];
+    int splits[3];
+    unsigned first[4];                               // first workgroup of each, and their number
+};
+__global__ __launch_bounds__(256) void linear_grad_reduce_kernel(GradSums g)
+{
+    const int which = blockIdx.x >= g.first[2] ? 2 : blockIdx.x >= g.first[1] ? 1 : 0;
+    const long i = ((long)(blockIdx.x - g.first[which]) * 256 + threadIdx.x) * 4, count = g.count[which];
     if (i >= count) return;
+    const float *const part = g.part[which];
+    const int splits = g.splits[which];
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
     for (int s = 0; s < splits; ++s) {
         const float4 u = *(const float4 *)(part + s * count + i);
         v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
     }
-    *(uint2 *)(out + i) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+    *(uint2 *)(g.out[which] + i) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
 }
 
 // bf16 rows [rows, cols] of codes in fragment order and their scales: sixteen channels a thread
@@ -325,69 +409,112 @@ __global__ __launch_bounds__(256) void restore_rows_kernel(const uint8_t *__rest
 }
 
 namespace {
-template <int T, bool TURN>
-hipError_t launch_grad(const void *A, int lda, const void *B, int M, int cols, int K, int splits, void *C, float *part, float *part_db, hipStream_t st)
-{
-    const int n_mt = (M + 64 * T - 1) / (64 * T), n_nt = (cols + 64 * T - 1) / (64 * T);
-    const long tiles = (long)n_mt * n_nt, total = tiles * splits;
-    if (total > 0x7FFFFFF0L) return hipErrorInvalidValue;
-    const int steps = (K + kStepK - 1) / kStepK, k_split = (steps + splits - 1) / splits * kStepK;
-    linear_grad_kernel<T, T, TURN><<<(unsigned)xcd_grid(total), 256, 0, st>>>((const uint16_t *)A, lda, (const uint8_t *)B, M, cols, K, k_split,
-                                                                              n_nt, (int)tiles, (int)total, (uint16_t *)C, part, part_db);
-    return hipGetLastError();
-}
-hipError_t launch_restore_turned(const void *codes, const float *scales, int rows, int cols, void *B, hipStream_t st)
-{
-    const long waves = (long)((rows + 31) / 32) * (cols / 128);
-    restore_turned_kernel<<<(unsigned)((waves + 3) / 4), 256, 0, st>>>((const uint8_t *)codes, scales, rows, cols, (uint8_t *)B);
-    return hipGetLastError();
-}
 long tiles_of(int M, int cols, int size) { return (long)((M + size - 1) / size) * ((cols + size - 1) / size); }
 
-// Tiles and splits of dW: enough workgroups for the chip, each split with at least eight steps, none without steps.
-struct GradPlan { int wide, splits; };
-GradPlan dw_plan(int N, int d_in, int d_out)
+// splits of `steps` steps into at most `most`, none without steps
+int even_splits(int steps, long most)
 {
+    if (most < 1) most = 1;
+    const int per = (int)((steps + most - 1) / most);
+    return steps ? (steps + per - 1) / per : 0;
+}
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+// Tiles and splits.  256 x 256 tiles reach 1.2 PFLOP/s, 128 x 128 tiles 0.85, where either fills the chip; what speaks for the
+// small ones is that a sum split less often leaves fewer partials (fp32, written and read again).
+//   dx  wide from 160 tiles on: 10992 x 1024 (172 wide tiles, 688 narrow ones) takes the same either way; else narrow, and split where
+//       there are fewer than 256 (few tokens), into parts of at least eight steps
+//   dW  wide where eight splits are enough for 256 workgroups (1024 x 1024 over 10992 tokens: 64 narrow tiles in 8 splits 32 us and 6 for
+//       the partials, 16 wide ones in 16 splits 34 and 11)
+struct Plan {
+    bool wide_x, wide_w;
+    int splits_x, splits_w;
+    size_t off_bx, off_part_x, off_part_w, off_part_db, total;                   // the operand of dx comes first
+};
+Plan make_plan(int N, int d_in, int d_out)
+{
+    Plan p;
+    p.wide_x = tiles_of(N, d_in, 256) >= 160;
+    const long tx = tiles_of(N, d_in, 128);
+    p.splits_x = p.wide_x || !N ? 1 : even_splits((d_out + kStepK - 1) / kStepK, tx >= 256 ? 1 : std::min(256 / tx, (long)(d_out / (8 * kStepK))));
     const int steps = (N + kStepK - 1) / kStepK;
-    GradPlan p;
-    p.wide = tiles_of(d_out, d_in, 256) * (steps / 8) >= 256;
-    long s = p.wide ? 256 / tiles_of(d_out, d_in, 256) : 512 / tiles_of(d_out, d_in, 128);
-    s = s > steps / 8 ? steps / 8 : s;
-    s = s < 1 ? 1 : s;
-    p.splits = steps ? (int)((steps + (steps + s - 1) / s - 1) / ((steps + s - 1) / s)) : 0;
+    const long tw = tiles_of(d_out, d_in, 256);
+    p.wide_w = tw >= 32 && tw * (steps / 8) >= 256;
+    p.splits_w = even_splits(steps, std::min(p.wide_w ? 256 / tw : 512 / tiles_of(d_out, d_in, 128), (long)steps / 8));
+    p.off_bx = (size_t)((d_out + 31) / 32) * 64 * d_in;
+    p.off_part_x = p.off_bx + (size_t)((N + 31) / 32) * 64 * d_in;
+    p.off_part_w = p.off_part_x + (p.splits_x > 1 ? up256((size_t)p.splits_x * N * d_in * 4) : 0);
+    p.off_part_db = p.off_part_w + (p.splits_w > 1 ? up256((size_t)p.splits_w * d_out * d_in * 4) : 0);
+    p.total = p.off_part_db + (p.splits_w > 1 ? up256((size_t)p.splits_w * d_out * 4) : 0);
     return p;
+}
+
+bool set_product(GradProduct &g, bool wide, int splits)
+{
+    const int size = wide ? 256 : 128, steps = (g.K + kStepK - 1) / kStepK;
+    const long tiles = tiles_of(g.M, g.cols, size), total = tiles * splits;
+    g.n_nt = (g.cols + size - 1) / size;
+    g.tiles = (int)tiles;
+    g.total = (int)total;
+    g.k_split = (steps + splits - 1) / splits * kStepK;
+    return total <= 0x3FFFFFF0L;
+}
+hipError_t launch_products(bool wide, const GradProduct &w, const GradProduct &x, hipStream_t st)
+{
+    const unsigned grid_w = w.total ? (unsigned)xcd_grid(w.total) : 0, grid = grid_w + (x.total ? (unsigned)xcd_grid(x.total) : 0);
+    if (wide) linear_grad_kernel<4><<<grid, 256, 0, st>>>(w, x, grid_w);
+    else      linear_grad_kernel<2><<<grid, 256, 0, st>>>(w, x, grid_w);
+    return hipGetLastError();
 }
 }  // namespace
 
-int linear_grad_splits(int N, int d_in, int d_out) { return dw_plan(N, d_in, d_out).splits; }
+size_t linear_grad_workspace(int N, int d_in, int d_out) { return make_plan(N, d_in, d_out).total; }
 
-size_t linear_grad_turned_bytes(int rows, int cols) { return (size_t)((rows + 31) / 32) * 32 * cols * 2; }
-
-hipError_t launch_linear_dx(const void *dy, const void *w8, const float *sw, int N, int d_in, int d_out, void *dx, void *turned, hipStream_t st)
+hipError_t launch_linear_grad(const void *dy, const void *x8, const float *sx, const void *W, int N, int d_in, int d_out, void *dx, void *dW, void *db,
+                              void *workspace, hipStream_t st)
 {
-    const hipError_t e = launch_restore_turned(w8, sw, d_out, d_in, turned, st);
-    if (e != hipSuccess) return e;
-    if (tiles_of(N, d_in, 256) >= 160) return launch_grad<4, false>(dy, d_out, turned, N, d_in, d_out, 1, dx, nullptr, nullptr, st);
-    return launch_grad<2, false>(dy, d_out, turned, N, d_in, d_out, 1, dx, nullptr, nullptr, st);
-}
-
-hipError_t launch_linear_dw(const void *dy, const void *x8, const float *sx, int N, int d_in, int d_out, void *dW, void *db, void *turned, float *part, hipStream_t st)
-{
-    const GradPlan p = dw_plan(N, d_in, d_out);
-    const int splits = p.splits;
-    const long count = (long)d_out * d_in;
-    float *const part_db = part + (size_t)splits * count;
-    if (splits) {
-        hipError_t e = launch_restore_turned(x8, sx, N, d_in, turned, st);
+    const Plan p = make_plan(N, d_in, d_out);
+    char *const ws = (char *)workspace;
+    GradSums sums = {};
+    auto add = [&](int i, const float *part, void *out, long count, int splits) {
+        sums.part[i] = part; sums.out[i] = (uint16_t *)out; sums.count[i] = count; sums.splits[i] = splits;
+    };
+    if (N > 0) {
+        uint8_t *const bw = (uint8_t *)ws, *const bx = (uint8_t *)ws + p.off_bx;
+        const int spans = d_in / 128;
+        const long w_blocks = dx ? (long)((d_out + 31) / 32) * ((spans + 3) / 4) : 0, x_blocks = dW ? ((long)((N + 31) / 32) * spans + 3) / 4 : 0;
+        if (w_blocks + x_blocks > 0x7FFFFFFFL) return hipErrorInvalidValue;
+        grad_operands_kernel<<<(unsigned)(w_blocks + x_blocks), 256, 0, st>>>((const uint16_t *)W, d_out, bw, (unsigned)w_blocks, (const uint8_t *)x8, sx, N, bx, d_in);
+        hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        e = p.wide ? launch_grad<4, true>(dy, d_out, turned, d_out, d_in, N, splits, nullptr, part, db ? part_db : nullptr, st)
-                   : launch_grad<2, true>(dy, d_out, turned, d_out, d_in, N, splits, nullptr, part, db ? part_db : nullptr, st);
+        GradProduct x = {}, w = {};
+        if (dx) {
+            x.A = (const uint16_t *)dy; x.B = bw; x.lda = d_out; x.M = N; x.cols = d_in; x.K = d_out; x.C = (uint16_t *)dx;
+            x.part = p.splits_x > 1 ? (float *)(ws + p.off_part_x) : nullptr;
+            if (!set_product(x, p.wide_x, p.splits_x)) return hipErrorInvalidValue;
+            if (x.part) add(0, x.part, dx, (long)N * d_in, p.splits_x);
+        }
+        if (dW) {
+            w.A = (const uint16_t *)dy; w.B = bx; w.lda = d_out; w.M = d_out; w.cols = d_in; w.K = N; w.C = (uint16_t *)dW; w.db = (uint16_t *)db;
+            w.part = p.splits_w > 1 ? (float *)(ws + p.off_part_w) : nullptr;
+            w.part_db = (float *)(ws + p.off_part_db);
+            if (!set_product(w, p.wide_w, p.splits_w)) return hipErrorInvalidValue;
+            if (w.part) add(1, w.part, dW, (long)d_out * d_in, p.splits_w);
+            if (w.part && db) add(2, w.part_db, db, d_out, p.splits_w);
+        }
+        if (dx && dW && p.wide_x != p.wide_w) {
+            const GradProduct none = {};
+            if ((e = launch_products(p.wide_w, w, none, st)) != hipSuccess) return e;
+            e = launch_products(p.wide_x, none, x, st);
+        } else e = launch_products(dW ? p.wide_w : p.wide_x, w, x, st);
         if (e != hipSuccess) return e;
+    } else {                                         // no tokens: sums of nothing
+        if (dW) add(1, nullptr, dW, (long)d_out * d_in, 0);
+        if (db) add(2, nullptr, db, d_out, 0);
     }
-    linear_grad_reduce_kernel<<<(unsigned)((count / 4 + 255) / 256), 256, 0, st>>>(part, splits, count, (uint16_t *)dW);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !db) return e;
-    linear_grad_reduce_kernel<<<(unsigned)((d_out / 4 + 255) / 256), 256, 0, st>>>(part_db, splits, d_out, (uint16_t *)db);
+    for (int i = 0; i < 3; ++i) sums.first[i + 1] = sums.first[i] + (unsigned)((sums.count[i] / 4 + 255) / 256);
+    if (!sums.first[3]) return hipSuccess;
+    linear_grad_reduce_kernel<<<sums.first[3], 256, 0, st>>>(sums);
     return hipGetLastError();
 }
 

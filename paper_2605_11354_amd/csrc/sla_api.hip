@@ -505,8 +505,8 @@ sla_status_t check_buffer(const char *name, const void *buf, size_t bytes, size_
     if (bytes < need) return fail(SLA_ERR_WORKSPACE, "%s has %zu bytes, %zu needed", name, bytes, need);
     return SLA_OK;
 }
-// Workspace of the layer's training calls: codes and scales of W, the restored operand of dx and then of dW, partial sums of dW and db.
-struct LinGradPlan { size_t off_sw, off_turned, off_part, total; };
+// Workspace of the layer's training calls: codes and scales of W (forward), or what the gradients' kernels need.
+struct LinGradPlan { size_t off_sw, total; };
 sla_status_t make_lin_grad_plan(int32_t N, int32_t d_in, int32_t d_out, LinGradPlan &gp)
 {
     LinPlan lp;
@@ -515,9 +515,8 @@ sla_status_t make_lin_grad_plan(int32_t N, int32_t d_in, int32_t d_out, LinGradP
     if ((double)N * d_out >= 4.0e9) return fail(SLA_ERR_UNSUPPORTED, "gradient of 4e9 values or more");
     if (d_out > 1 << 22) return fail(SLA_ERR_UNSUPPORTED, "d_out = %d; at most 2^22 are implemented", d_out);       // 256 rows of dy within 2 GB
     gp.off_sw = align_up((size_t)d_out * d_in, 256);
-    gp.off_turned = gp.off_sw + align_up((size_t)d_out * sizeof(float), 256);
-    gp.off_part = gp.off_turned + sla::linear_grad_turned_bytes(N > d_out ? N : d_out, d_in);
-    gp.total = gp.off_part + align_up((size_t)sla::linear_grad_splits(N, d_in, d_out) * d_out * ((size_t)d_in + 1) * sizeof(float), 256);
+    const size_t forward = gp.off_sw + align_up((size_t)d_out * sizeof(float), 256), backward = sla::linear_grad_workspace(N, d_in, d_out);
+    gp.total = forward > backward ? forward : backward;
     return SLA_OK;
 }
 }  // namespace
@@ -588,15 +587,9 @@ sla_status_t sla_fp8_linear_grad(const void *dy, const void *checkpoint, size_t 
         if (dW && (s = check_buffer("checkpoint", checkpoint, checkpoint_bytes, cp.total)) != SLA_OK) return s;
         if ((s = check_buffer("workspace", workspace, workspace_bytes, gp.total)) != SLA_OK) return s;
     }
-    hipStream_t st = (hipStream_t)stream;
-    if (dx && N > 0) {
-        float *const sw = at<float>(workspace, gp.off_sw);
-        SLA_HIP(sla::launch_quantise_rows(nullptr, 0, nullptr, nullptr, W, d_out, workspace, sw, d_in, st));
-        SLA_HIP(sla::launch_linear_dx(dy, workspace, sw, N, d_in, d_out, dx, at<void>(workspace, gp.off_turned), st));
-    }
-    if (dW)
-        SLA_HIP(sla::launch_linear_dw(dy, checkpoint, (const float *)((const char *)checkpoint + cp.off_scales), N, d_in, d_out, dW, db,
-                                      at<void>(workspace, gp.off_turned), at<float>(workspace, gp.off_part), st));
+    if ((dx && N > 0) || dW)
+        SLA_HIP(sla::launch_linear_grad(dy, checkpoint, (const float *)((const char *)checkpoint + cp.off_scales), W, N, d_in, d_out, dx, dW, db,
+                                        workspace, (hipStream_t)stream));
     return SLA_OK;
 }
 

@@ -92,13 +92,11 @@ int fp8_gemm_qkv_token_tile(int M, int H);
 hipError_t launch_fp8_gemm_qkv(const void *A8, const float *sa, const void *W8, const float *sw, const void *bias, int B, int N, int H, int K,
                                int bq, void *const codes[3], float *const scales[3], hipStream_t st);
 
-// Gradients of the FP8 layer from the codes and scales of its forward (k_linear_grad.hip); cols, rows as launch_quantise_rows takes them
-// turned: linear_grad_turned_bytes(d_out (dx) or N (dW), d_in) bytes of scratch
-size_t linear_grad_turned_bytes(int rows, int cols);
-hipError_t launch_linear_dx(const void *dy, const void *w8, const float *sw, int N, int d_in, int d_out, void *dx, void *turned, hipStream_t st);
-// part: linear_grad_splits(...) * d_out * (d_in + 1) floats of scratch; db may be NULL; N = 0 gives zeros
-int linear_grad_splits(int N, int d_in, int d_out);
-hipError_t launch_linear_dw(const void *dy, const void *x8, const float *sx, int N, int d_in, int d_out, void *dW, void *db, void *turned, float *part, hipStream_t st);
+// Gradients of the FP8 layer (k_linear_grad.hip) from dy bf16 [N, d_out], the kept codes and scales of x as launch_quantise_rows leaves them
+// (dW, db) and W bf16 (dx).  dx, dW, db may be NULL, db is with dW only; N = 0 gives zeros of dW and db.
+size_t linear_grad_workspace(int N, int d_in, int d_out);
+hipError_t launch_linear_grad(const void *dy, const void *x8, const float *sx, const void *W, int N, int d_in, int d_out, void *dx, void *dW, void *db,
+                              void *workspace, hipStream_t st);
 // X bf16 [rows, cols] = codes (fragment order) times the scales of their rows
 hipError_t launch_restore_rows(const void *codes, const float *scales, long rows, int cols, void *X, hipStream_t st);
 
