@@ -274,7 +274,7 @@ typedef struct {
     int32_t pairing;             /* sla_pairing_t */
     int32_t pos_per_item;        /* positions: 0: [N, axes], the same for every item; 1: [B, N, axes] */
     int32_t layout;              /* sla_layout_t of the outputs Q, K, V (and of dQ, dK, dV) */
-    float   eps;                 /* > 0 unless SLA_NORM_NONE; the squares are summed in fp32, so |x| must stay below 2^60 */
+    float   eps;                 /* a normal fp32 number > 0 unless SLA_NORM_NONE; the squares are summed in fp32, so |x| must stay below 2^60 */
     double  base;                /* >= 1, finite; ignored with axes = 0 */
     int64_t batch_stride, token_stride, head_stride;
                                  /* elements between the rows of q, k, v (and of dq, dk, dv): multiples of 8, at least 64, and

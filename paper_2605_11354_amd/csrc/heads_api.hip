@@ -2,6 +2,7 @@
 #include "api_util.hpp"
 #include "sla_kernels.hpp"
 
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 
@@ -11,7 +12,7 @@ using sla::fail;
 
 namespace {
 
-constexpr double kTwoPi = 6.283185307179586476925286766559;
+constexpr double kQuarterTurn = 1.5707963267948966192313216916398;
 
 sla_status_t make_args(const sla_heads_params_t *p, sla::HeadsArgs &a)
 {
@@ -26,7 +27,7 @@ sla_status_t make_args(const sla_heads_params_t *p, sla::HeadsArgs &a)
     if (p->pairing != SLA_PAIR_HALVES && p->pairing != SLA_PAIR_ADJACENT) return fail(SLA_ERR_INVALID_ARG, "unknown pairing %d", p->pairing);
     if (p->pos_per_item != 0 && p->pos_per_item != 1) return fail(SLA_ERR_INVALID_ARG, "pos_per_item must be 0 or 1");
     if (p->layout != SLA_LAYOUT_BHND && p->layout != SLA_LAYOUT_BNHD) return fail(SLA_ERR_INVALID_ARG, "unknown layout %d", p->layout);
-    if (p->norm != SLA_NORM_NONE && !(p->eps > 0.f && std::isfinite(p->eps))) return fail(SLA_ERR_INVALID_ARG, "eps must be finite and > 0");
+    if (p->norm != SLA_NORM_NONE && !(p->eps >= FLT_MIN && std::isfinite(p->eps))) return fail(SLA_ERR_INVALID_ARG, "eps must be a finite normal number > 0");
     if (p->axes && !(p->base >= 1.0 && std::isfinite(p->base))) return fail(SLA_ERR_INVALID_ARG, "base must be finite and >= 1");
     memset(&a, 0, sizeof a);
     a.B = p->B; a.H = p->H; a.N = p->N;
@@ -50,7 +51,7 @@ sla_status_t make_args(const sla_heads_params_t *p, sla::HeadsArgs &a)
     const sla::RowMap out = sla::make_rowmap(p->layout == SLA_LAYOUT_BNHD, p->H, p->N);
     a.obs = out.bs; a.ots = out.ts; a.ohs = out.hs;
     if (p->axes)
-        for (int j = 0, per = 32 / p->axes; j < 32; ++j) a.turn[j] = std::pow(p->base, -(double)(j % per) / per) / kTwoPi;
+        for (int j = 0, per = 32 / p->axes; j < 32; ++j) a.turn[j] = std::pow(p->base, -(double)(j % per) / per) / kQuarterTurn;
     return SLA_OK;
 }
 

@@ -121,7 +121,7 @@ struct HeadsArgs {
     int norm, per_head, axes, adjacent, pos_per_item;     // norm: 0 none, 1 RMS, 2 layer
     float eps;
     int chunk, splits;          // set by the launch: (tensor, head) items of a workgroup, workgroups of a token block
-    double turn[32];            // turns per unit of position, of every angle of the table (k_heads.hip)
+    double turn[32];            // quarter turns per unit of position, of every angle of the table (k_heads.hip)
 };
 struct HeadsGrads {
     const uint16_t *g[3];       // gradients of y
