@@ -19,9 +19,9 @@ SOURCES = ["sla_api.hip", "k_classify.hip", "k_states.hip", "k_aggregate.hip", "
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-ffp-contract=off", "-Wall", "-Wextra",
          "-Wno-unused-parameter", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-mllvm", "-amdgpu-mfma-vgpr-form=1"]   # MFMA accumulators stay in VGPRs: no AGPR copy traffic
-# The wide tiles of this file hold 256 accumulators a lane, which only the other half of the register file has room for (with
+# The wide tiles of these files hold 256 accumulators a lane, which only the other half of the register file has room for (with
 # the flag its main loop copies two hundred registers a step)
-AGPR_FORM = ["k_linear_grad.hip"]
+AGPR_FORM = ["k_linear_grad.hip", "k_mxfp4.hip"]
 
 
 def _hipcc() -> str:

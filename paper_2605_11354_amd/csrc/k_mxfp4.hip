@@ -34,6 +34,13 @@ __device__ __forceinline__ uint32_t codes8(uint4 u, float scale)
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, u.z), scale, 2);
     return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, u.w), scale, 3);
 }
+// 256 bytes global -> LDS: lane l moves the dword at base + voff(l) to LDS byte lds_addr + 4 l (otherwise as copy_1k_to_lds)
+__device__ __forceinline__ void copy_256_to_lds(const uint8_t *base, uint32_t voff, uint32_t lds_addr)
+{
+    uint32_t saved_m0;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b32 m0, %0"
+                 : "=&s"(saved_m0) : "v"(voff), "s"(base), "s"(lds_addr) : "memory");
+}
 __device__ __forceinline__ float scale_value(uint32_t s) { return __uint_as_float(s ? s << 23 : 0x00400000u); }
 }  // namespace
 
@@ -69,95 +76,134 @@ __global__ __launch_bounds__(256) void dequantise_mxfp4_kernel(const uint32_t *_
 }
 
 // Large products.  A [M, K] tokens, W [O, K] channels: codes (K / 2 bytes a row) and scales (K / 32 bytes a row) as they lie.
-// Workgroup tile 64 TB tokens x 128 channels, four waves as 2 x 2; steps of 128 elements: 64 bytes and one dword of
-// scales of every row.  In LDS the 16-byte piece c of row r is at position c ^ (r / 4 % 4): sixteen rows' reads of one piece
-// meet all banks once.  D[o][i] (W is the first operand): a lane's four consecutive registers are consecutive channels.
-template <int TB>
-__global__ __launch_bounds__(256, 2) void mxfp4_gemm_kernel(const uint8_t *__restrict__ A, const uint8_t *__restrict__ As, const uint8_t *__restrict__ W,
+// Workgroup tile 64 TM tokens x 64 TN channels, four waves as 2 x 2.  Steps of 128 elements: 64 bytes and one dword of scales of
+// every row, copied straight to LDS, four stages, copies three steps ahead.  In LDS the 16-byte piece c of row r is at position
+// c ^ (r / 4 % 4): sixteen rows' reads of one piece meet all banks once.  A step has two parts of 64 elements (one matrix instruction
+// deep); the operands of a part are read while the products of the one before run, and reads and copies stand between the products,
+// because a wave of the largest tile is alone on its SIMD.  The one barrier of a step stands before the products of its second part,
+// whose operands are in registers by then.
+// D[channel][token] (W is the first operand): a lane's four consecutive registers are consecutive channels.
+template <int TM, int TN>
+__global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void mxfp4_gemm_kernel(const uint8_t *__restrict__ A, const uint8_t *__restrict__ As, const uint8_t *__restrict__ W,
                                                             const uint8_t *__restrict__ Ws, const uint16_t *__restrict__ bias, int M, int O, int K,
                                                             int n_ot, int total, uint16_t *__restrict__ Y)
 {
-    constexpr int kTok = 64 * TB, kRows = kTok + 128, kStage = kRows * 68;       // codes of all rows, then their scales
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * kStage];
+    constexpr int BM = 64 * TM, BN = 64 * TN, kRows = BM + BN, kStage = kRows * 68, kStages = 4;      // codes of all rows, tokens first, then their scales
+    constexpr int kCodes = kRows / 64, kScales = (kRows / 64 + 3) / 4, kCopies = kCodes + kScales;       // copies a wave makes in a step: of 1 KB, of 256 bytes
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[kStages * kStage];
     const int item = (int)xcd_remap(blockIdx.x, total);
     if (item >= total) return;
     const int it = (int)((unsigned)item / (unsigned)n_ot), ot = item - it * n_ot;
-    const int i0 = it * kTok, o0 = ot * 128;
+    const int i0 = it * BM, o0 = ot * BN;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wo = (wave >> 1) * 64, wi = (wave & 1) * (32 * TB);
+    const int wi = (wave & 1) * 32 * TM, wo = (wave >> 1) * 32 * TN;
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
 
-    // what a thread brings in: TB pieces of tokens' rows and two of channels' rows (row id / 4, piece id % 4), one dword of
-    // scales of each; rows past the end repeat the last one: their results are not stored
-    const uint8_t *pa[TB], *pw[2];
+    // copy x of wave w: sixteen rows' pieces from row 16 (w kCodes + x) of the stage on, or the scales of 64 rows; rows past the end repeat
+    // the last one: their results are not stored
+    const uint8_t *pc[kCodes], *ps[kScales];
+    uint32_t vc[kCodes], vs[kScales];
+    auto clamped = [&](int r) { return r < BM ? min(r, M - 1 - i0) : min(r - BM, O - 1 - o0); };       // row of the tile's tokens or channels
 #pragma unroll
-    for (int x = 0; x < TB; ++x) pa[x] = A + (size_t)min(i0 + x * 64 + (tid >> 2), M - 1) * (K / 2) + (tid & 3) * 16;
+    for (int x = 0; x < kCodes; ++x) {
+        const int first = (wave * kCodes + x) * 16, r = first + (lane >> 2);                             // uniform: sixteen rows are of one matrix
+        pc[x] = first < BM ? A + (size_t)i0 * (K / 2) : W + (size_t)o0 * (K / 2);
+        vc[x] = (uint32_t)clamped(r) * (uint32_t)(K / 2) + (((lane & 3) ^ (r >> 2)) & 3) * 16;
+    }
+    int sr[kScales];                                                                                     // first row of a copy of scales (64 x 1 tiles: two waves make the same)
 #pragma unroll
-    for (int x = 0; x < 2; ++x) pw[x] = W + (size_t)min(o0 + x * 64 + (tid >> 2), O - 1) * (K / 2) + (tid & 3) * 16;
-    const uint8_t *const pas = As + (size_t)min(i0 + min(tid, kTok - 1), M - 1) * (K / 32);
-    const uint8_t *const pws = Ws + (size_t)min(o0 + (tid & 127), O - 1) * (K / 32);
-    const int at = (tid >> 2) * 64 + (((tid & 3) ^ (tid >> 4)) & 3) * 16;        // place of the first piece; others 64 rows on
-    i32x4 ra[TB], rw[2];
-    uint32_t sca, scw;
-    auto load = [&](int k) {
-#pragma unroll
-        for (int x = 0; x < TB; ++x) ra[x] = *(const i32x4 *)(pa[x] + k / 2);
-#pragma unroll
-        for (int x = 0; x < 2; ++x) rw[x] = *(const i32x4 *)(pw[x] + k / 2);
-        sca = *(const uint32_t *)(pas + k / 32);
-        scw = *(const uint32_t *)(pws + k / 32);
+    for (int x = 0; x < kScales; ++x) {
+        sr[x] = min(wave * kScales + x, kRows / 64 - 1) * 64;
+        ps[x] = sr[x] < BM ? As + (size_t)i0 * (K / 32) : Ws + (size_t)o0 * (K / 32);
+        vs[x] = (uint32_t)clamped(sr[x] + lane) * (uint32_t)(K / 32);
+    }
+    auto copy_one = [&](int s, int x) {
+        const uint32_t to = lds_base + (s & (kStages - 1)) * kStage;
+        if (x < kCodes) copy_1k_to_lds(pc[x] + (size_t)s * 64, vc[x], to + (wave * kCodes + x) * 1024);
+        else copy_256_to_lds(ps[x - kCodes] + (size_t)s * 4, vs[x - kCodes], to + kRows * 64 + sr[x - kCodes] * 4);
     };
-    auto store = [&](uint8_t *st) {
+
+    f32x16 acc[TN][TM];
 #pragma unroll
-        for (int x = 0; x < TB; ++x) *(i32x4 *)(st + x * 4096 + at) = ra[x];
+    for (int a = 0; a < TN; ++a)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) *(i32x4 *)(st + kTok * 64 + x * 4096 + at) = rw[x];
-        if (tid < kTok) *(uint32_t *)(st + kRows * 64 + tid * 4) = sca;
-        if (tid < 128) *(uint32_t *)(st + kRows * 64 + (kTok + tid) * 4) = scw;
-    };
-    f32x16 acc[2][TB];
-#pragma unroll
-    for (int a = 0; a < 2; ++a)
-#pragma unroll
-        for (int b = 0; b < TB; ++b)
+        for (int b = 0; b < TM; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[a][b][e] = 0.f;
-    auto frag = [&](const uint8_t *st, int row0, int t) {
-        const int r = row0 + l32;
-        const i32x4 u = *(const i32x4 *)(st + r * 64 + (((2 * t + g) ^ (l32 >> 2)) & 3) * 16);
-        return i32x8{u[0], u[1], u[2], u[3], 0, 0, 0, 0};
+    constexpr int kOps = TM + TN;                                                // operands of a part: TN of W, then TM of x
+    i32x4 op[2][kOps];
+    int sc[kOps], next_sc[kOps];
+    auto row_of = [&](int x) { return (x < TN ? BM + wo + 32 * x : wi + 32 * (x - TN)) + l32; };
+    auto read_op = [&](int set, int s, int t, int x) {
+        op[set][x] = *(const i32x4 *)(smem + (s & (kStages - 1)) * kStage + row_of(x) * 64 + (((2 * t + g) ^ (l32 >> 2)) & 3) * 16);
     };
-    auto scale = [&](const uint8_t *st, int row0) { return (int)(*(const uint32_t *)(st + kRows * 64 + (row0 + l32) * 4) >> (8 * g)); };
-
-    const int steps = K / 128;
-    load(0);
-    store(smem);
-    __syncthreads();
-    for (int s = 0; s < steps; ++s) {
-        const uint8_t *const st = smem + (s & 1) * kStage;
-        if (s + 1 < steps) load((s + 1) * 128);
-        int sa[TB], sw[2];
+    auto read_scale = [&](int s, int x) { return *(const int *)(smem + (s & (kStages - 1)) * kStage + kRows * 64 + row_of(x) * 4); };
+    auto mine = [&](int dword) { return (int)((uint32_t)dword >> (8 * g)); };    // this half's two blocks of the step: bytes 0 and 2
+    auto wide = [](i32x4 u) { return i32x8{u[0], u[1], u[2], u[3], 0, 0, 0, 0}; };
+    // the products of a part; what `between` does is spread over the gaps behind them
+    auto multiply = [&](auto part, auto between) {
+        constexpr int t = decltype(part)::value;
 #pragma unroll
-        for (int b = 0; b < TB; ++b) sa[b] = scale(st, wi + 32 * b);
-#pragma unroll
-        for (int a = 0; a < 2; ++a) sw[a] = scale(st, kTok + wo + 32 * a);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            i32x8 wf[2], af[TB];
-#pragma unroll
-            for (int a = 0; a < 2; ++a) wf[a] = frag(st, kTok + wo + 32 * a, t);
-#pragma unroll
-            for (int b = 0; b < TB; ++b) af[b] = frag(st, wi + 32 * b, t);
-#pragma unroll
-            for (int b = 0; b < TB; ++b)
-#pragma unroll
-                for (int a = 0; a < 2; ++a)
-                    acc[a][b] = t == 0 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[a], af[b], acc[a][b], kFp4, kFp4, 0, sw[a], 0, sa[b])
-                                       : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[a], af[b], acc[a][b], kFp4, kFp4, 2, sw[a], 2, sa[b]);
+        for (int i = 0; i < TM * TN; ++i) {
+            const int a = i / TM, b = i % TM;
+            acc[a][b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(op[t][a]), wide(op[t][TN + b]), acc[a][b], kFp4, kFp4, 2 * t, sc[a], 2 * t, sc[TN + b]);
+            __builtin_amdgcn_sched_barrier(0);
+            between(i);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        if (s + 1 < steps) store(smem + ((s + 1) & 1) * kStage);
-        __syncthreads();
+    };
+    auto spread = [](int i, int count, auto f) {     // the share of `count` things that goes behind product i
+#pragma unroll
+        for (int x = 0; x < count; ++x)
+            if (x * (TM * TN) / count == i) f(x);
+    };
+    using Part0 = std::integral_constant<int, 0>;
+    using Part1 = std::integral_constant<int, 1>;
+    using Two = std::integral_constant<int, 2>;
+    using Yes = std::true_type;
+    using No = std::false_type;
+    const int steps = K / 128;
+    // AHEAD: later steps than the next one whose copies may still be under way
+    auto step = [&](int s, auto copies, auto ahead, auto last) {
+        constexpr bool kCopy = decltype(copies)::value, kLast = decltype(last)::value;
+        multiply(Part0{}, [&](int i) {
+            spread(i, kOps, [&](int x) { read_op(1, s, 1, x); });
+            if constexpr (kCopy) spread(i, kCopies, [&](int x) { copy_one(s + 3, x); });
+        });
+        if constexpr (!kLast) {
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(ahead)::value * kCopies) : "memory");
+            lds_barrier();
+        }
+        multiply(Part1{}, [&](int i) {
+            if constexpr (!kLast) {
+                spread(i, kOps, [&](int x) { read_op(0, s + 1, 0, x); });
+                spread(i, kOps, [&](int x) { next_sc[x] = read_scale(s + 1, x); });
+            }
+        });
+        if constexpr (!kLast) {
+#pragma unroll
+            for (int x = 0; x < kOps; ++x) sc[x] = mine(next_sc[x]);
+        }
+    };
+
+    for (int s = 0; s < min(steps, 3); ++s)
+#pragma unroll
+        for (int x = 0; x < kCopies; ++x) copy_one(s, x);
+    if (steps > 2)       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kCopies) : "memory");
+    else if (steps == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kCopies) : "memory");
+    else                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    lds_barrier();
+#pragma unroll
+    for (int x = 0; x < kOps; ++x) {
+        read_op(0, 0, 0, x);
+        sc[x] = mine(read_scale(0, x));
     }
+    int s = 0;
+    for (; s + 3 < steps; ++s) step(s, Yes{}, Two{}, No{});
+    if (s + 2 < steps) step(s++, No{}, Part1{}, No{});
+    if (s + 1 < steps) step(s++, No{}, Part0{}, No{});
+    step(s, No{}, Part0{}, Yes{});
 
     // register 4q + r of acc[a][b], lane (l32, g): channel 32 a + 8 q + 4 g + r, token 32 b + l32; v_permlane32_swap brings the
     // two halves of a 16-byte store together
@@ -167,7 +213,7 @@ __global__ __launch_bounds__(256, 2) void mxfp4_gemm_kernel(const uint8_t *__res
         hi = r[1];
     };
 #pragma unroll
-    for (int a = 0; a < 2; ++a)
+    for (int a = 0; a < TN; ++a)
 #pragma unroll
         for (int q = 0; q < 4; q += 2) {
             float bi[2][4];
@@ -176,7 +222,7 @@ __global__ __launch_bounds__(256, 2) void mxfp4_gemm_kernel(const uint8_t *__res
 #pragma unroll
                 for (int r = 0; r < 4; ++r) bi[h][r] = bias ? bf16_bits_to_f32(bias[min(o0 + wo + 32 * a + 8 * (q + h) + 4 * g + r, O - 1)]) : 0.f;
 #pragma unroll
-            for (int b = 0; b < TB; ++b) {
+            for (int b = 0; b < TM; ++b) {
                 const int i = i0 + wi + 32 * b + l32, o = o0 + wo + 32 * a + 8 * q + 8 * g;
                 const f32x16 &v = acc[a][b];
                 uint32_t x0 = pack_bf16(v[4 * q] + bi[0][0], v[4 * q + 1] + bi[0][1]), y0 = pack_bf16(v[4 * q + 2] + bi[0][2], v[4 * q + 3] + bi[0][3]);
@@ -273,14 +319,14 @@ template <int T> hipError_t launch_few(const void *X, const void *W, const void 
                                                                                   (const uint16_t *)bias, M, O, K, parts, (uint16_t *)Y);
     return hipGetLastError();
 }
-template <int TB>
+template <int TM, int TN>
 hipError_t launch_gemm(const void *A, const void *As, const void *W, const void *Ws, const void *bias, int M, int O, int K, void *Y, hipStream_t st)
 {
-    const int n_it = (M + 64 * TB - 1) / (64 * TB), n_ot = (O + 127) / 128;
+    const int n_it = (M + 64 * TM - 1) / (64 * TM), n_ot = (O + 64 * TN - 1) / (64 * TN);
     const long total = (long)n_it * n_ot;
     if (total > 0x7FFFFFF0L) return hipErrorInvalidValue;
-    mxfp4_gemm_kernel<TB><<<(unsigned)xcd_grid(total), 256, 0, st>>>((const uint8_t *)A, (const uint8_t *)As, (const uint8_t *)W, (const uint8_t *)Ws,
-                                                                     (const uint16_t *)bias, M, O, K, n_ot, (int)total, (uint16_t *)Y);
+    mxfp4_gemm_kernel<TM, TN><<<(unsigned)xcd_grid(total), 256, 0, st>>>((const uint8_t *)A, (const uint8_t *)As, (const uint8_t *)W, (const uint8_t *)Ws,
+                                                                         (const uint16_t *)bias, M, O, K, n_ot, (int)total, (uint16_t *)Y);
     return hipGetLastError();
 }
 }  // namespace
@@ -293,10 +339,10 @@ hipError_t launch_mxfp4_few(const void *X, const void *W, const void *Ws, const 
 
 hipError_t launch_mxfp4_gemm(const void *A, const void *As, const void *W, const void *Ws, const void *bias, int M, int O, int K, void *Y, hipStream_t st)
 {
-    const long n_ot = (O + 127) / 128;
-    if ((M + 255) / 256 * n_ot >= 512) return launch_gemm<4>(A, As, W, Ws, bias, M, O, K, Y, st);
-    if ((M + 127) / 128 * n_ot >= 400) return launch_gemm<2>(A, As, W, Ws, bias, M, O, K, Y, st);
-    return launch_gemm<1>(A, As, W, Ws, bias, M, O, K, Y, st);
+    const long wide = (long)((M + 255) / 256) * ((O + 255) / 256), n_ot = (O + 127) / 128;
+    if (wide >= 160) return launch_gemm<4, 4>(A, As, W, Ws, bias, M, O, K, Y, st);
+    if ((M + 127) / 128 * n_ot >= 400) return launch_gemm<2, 2>(A, As, W, Ws, bias, M, O, K, Y, st);
+    return launch_gemm<1, 2>(A, As, W, Ws, bias, M, O, K, Y, st);
 }
 
 }  // namespace sla

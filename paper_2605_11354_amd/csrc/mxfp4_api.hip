@@ -24,6 +24,7 @@ sla_status_t make_mx_plan(int32_t N, int32_t d_in, int32_t d_out, MxPlan &mp)
     if (d_in % 128 != 0) return fail(SLA_ERR_UNSUPPORTED, "d_in = %d; only multiples of 128 are implemented", d_in);
     if (d_out % 8 != 0) return fail(SLA_ERR_UNSUPPORTED, "d_out = %d; only multiples of 8 are implemented", d_out);
     if ((double)N * d_in >= 4.0e9 || (double)d_out * d_in >= 4.0e9 || (double)N * d_out >= 4.0e9) return fail(SLA_ERR_UNSUPPORTED, "matrix of 4e9 elements or more");
+    if (d_in > 1 << 24) return fail(SLA_ERR_UNSUPPORTED, "d_in = %d; at most 2^24 are implemented", d_in);       // 256 rows of codes within 2 GB
     mp.off_scales = align_up((size_t)N * d_in / 2, 256);
     mp.total = sla::mxfp4_few(N) ? 0 : mp.off_scales + align_up((size_t)N * d_in / 32, 256);
     return SLA_OK;
