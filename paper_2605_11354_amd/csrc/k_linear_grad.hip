@@ -14,7 +14,7 @@
 // a group 16 k after 16 k, 1 KB each, lane l's 16 bytes (column l % 32, k = 8 (l / 32) ..) one after the other; k past the end are
 // zeros up to a multiple of 32.  (Converted on the way to LDS instead, every tile of rows converts it again: four vector instructions
 // for each matrix instruction, 540 us instead of 30 for the restoring and what the products then take.)
-#include "sla_common.hpp"
+#include "gemm_common.hpp"
 #include "sla_kernels.hpp"
 
 #include <algorithm>
@@ -315,11 +315,6 @@ __device__ __forceinline__ void grad_tile(const GradProduct &p, int item, uint8_
     step(s, No{}, Ahead0{}, Yes{});
 
     // register 4q + r of acc[b][a], lane (l32, g): n = 32 b + 8 q + 4 g + r, m = 32 a + l32
-    auto swap32 = [](uint32_t &lo, uint32_t &hi) {                               // upper lanes of lo <-> lower lanes of hi
-        const auto r = __builtin_amdgcn_permlane32_swap(lo, hi, false, false);
-        lo = r[0];
-        hi = r[1];
-    };
 #pragma unroll
     for (int a = 0; a < TM; ++a) {
         const int m = m0 + wm + 32 * a + l32;
@@ -330,27 +325,23 @@ __device__ __forceinline__ void grad_tile(const GradProduct &p, int item, uint8_
                 else p.db[m] = (uint16_t)pack_bf16(v, v);
             }
         }
+        if (part) {
 #pragma unroll
-        for (int b = 0; b < TN; ++b) {
-            const f32x16 &v = acc[b][a];
-            if (part) {
+            for (int b = 0; b < TN; ++b)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
+                    const f32x16 &v = acc[b][a];
                     const int n = n0 + wn + 32 * b + 8 * q + 4 * g;
                     if (m < M && n < cols) *(float4 *)(part + ((size_t)split * M + m) * cols + n) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
                 }
-            } else {
-#pragma unroll
-                for (int q = 0; q < 4; q += 2) {
-                    uint32_t x0 = pack_bf16(v[4 * q], v[4 * q + 1]), y0 = pack_bf16(v[4 * q + 2], v[4 * q + 3]);
-                    uint32_t x1 = pack_bf16(v[4 * q + 4], v[4 * q + 5]), y1 = pack_bf16(v[4 * q + 6], v[4 * q + 7]);
-                    swap32(x0, x1);
-                    swap32(y0, y1);
-                    const int n = n0 + wn + 32 * b + 8 * q + 8 * g;
-                    if (m < M && n < cols) *(uint4 *)(p.C + (size_t)m * cols + n) = make_uint4(x0, y0, x1, y1);
-                }
-            }
         }
+    }
+    if (!part) {
+        lds_barrier();                               // everybody has read the last stage
+        store_tile<TM, TN>(smem + wave * kStoreBytes<TN>, [&](int b, int a, int q, float (&v)[4]) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = acc[b][a][4 * q + r];
+        }, lane, M - m0 - wm, cols - n0 - wn, p.C + (size_t)(m0 + wm) * cols + n0 + wn, (size_t)cols);
     }
 }
 

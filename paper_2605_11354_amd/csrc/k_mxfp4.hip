@@ -4,7 +4,7 @@
 // A block with an infinity or NaN gets s = 255 (NaN) and codes 0.  The linear layer
 //     y[i][o] = sum over blocks of 2^(sx + sw - 254) sum of c_x c_w + bias[o]
 // runs on the scaled matrix instructions, which take both scales beside the codes: products are exact, sums are fp32.
-#include "sla_common.hpp"
+#include "gemm_common.hpp"
 #include "sla_kernels.hpp"
 
 #include <type_traits>
@@ -34,28 +34,50 @@ __device__ __forceinline__ uint32_t codes8(uint4 u, float scale)
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, u.z), scale, 2);
     return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, u.w), scale, 3);
 }
-// 256 bytes global -> LDS: lane l moves the dword at base + voff(l) to LDS byte lds_addr + 4 l (otherwise as copy_1k_to_lds)
-__device__ __forceinline__ void copy_256_to_lds(const uint8_t *base, uint32_t voff, uint32_t lds_addr)
-{
-    uint32_t saved_m0;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b32 m0, %0"
-                 : "=&s"(saved_m0) : "v"(voff), "s"(base), "s"(lds_addr) : "memory");
-}
 __device__ __forceinline__ float scale_value(uint32_t s) { return __uint_as_float(s ? s << 23 : 0x00400000u); }
 }  // namespace
 
 // Four lanes to a block, 16 bytes of it each: 2 bytes in, 17/32 out per element, bound by HBM.
-__global__ __launch_bounds__(256) void quantise_mxfp4_kernel(const uint4 *__restrict__ X, long pieces, uint32_t *__restrict__ codes, uint8_t *__restrict__ scales)
+// BY_STEPS: both as the product below takes them, in steps of 128 elements, so that what a copy to LDS brings lies side by side:
+//     codes   of sixteen rows and a step 1 KB, row after row, steps after one another:  ((r / 16) steps + s) 1024 + (r % 16) 64
+//     scales  the dword of row r and step s at s rows + r                               (rows x steps dwords)
+// and the workgroups from first_w on bring the weights (O rows) into the same order.  As they lie by rows, K / 2 bytes apart, often a power
+// of two, the rows of a step come from one or two of the sixteen channels of the L2, and every dword of scales is a request of its own.
+struct WeightsIn {
+    const i32x4 *codes;
+    const uint32_t *scales;
+    i32x4 *codes_out;
+    uint32_t *scales_out;
+    int O;
+    unsigned first_w;
+};
+template <bool BY_STEPS>
+__global__ __launch_bounds__(256) void quantise_mxfp4_kernel(const uint4 *__restrict__ X, long pieces, uint32_t *__restrict__ codes, uint8_t *__restrict__ scales,
+                                                             int rows, int steps, WeightsIn w)
 {
     const long at = (long)blockIdx.x * 256 + threadIdx.x;      // pieces is a multiple of four: a block's lanes all work or all leave
+    if constexpr (BY_STEPS)
+        if (blockIdx.x >= w.first_w) {                         // four codes' pieces and a dword of scales to (row, step): 16 bytes a thread
+            const unsigned i = (blockIdx.x - w.first_w) * 256 + threadIdx.x, row = i / (4u * steps), q = i - row * 4u * steps, s = q >> 2;
+            if (row >= (unsigned)w.O) return;
+            w.codes_out[((size_t)(row >> 4) * steps + s) * 64 + (row & 15) * 4 + (q & 3)] = w.codes[i];
+            if ((q & 3) == 0) w.scales_out[(size_t)s * w.O + row] = w.scales[(size_t)row * steps + s];
+            return;
+        }
     if (at >= pieces) return;
     const uint4 u = X[at];
     uint32_t top = top_bits(u);
     top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0xB1, 0xf, 0xf, true));
     top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0x4E, 0xf, 0xf, true));
-    const uint32_t s = scale_byte(top);
-    codes[at] = s == 255 ? 0u : codes8(u, scale_value(s));
-    if ((at & 3) == 0) scales[at >> 2] = (uint8_t)s;
+    const uint32_t s = scale_byte(top), code = s == 255 ? 0u : codes8(u, scale_value(s));
+    if constexpr (BY_STEPS) {
+        const unsigned row = (unsigned)at / (16u * steps), q = (unsigned)at - row * 16u * steps, st = q >> 4;
+        codes[((size_t)(row >> 4) * steps + st) * 256 + (row & 15) * 16 + (q & 15)] = code;
+        if ((q & 3) == 0) scales[((size_t)st * rows + row) * 4 + (q >> 2 & 3)] = (uint8_t)s;
+    } else {
+        codes[at] = code;
+        if ((at & 3) == 0) scales[at >> 2] = (uint8_t)s;
+    }
 }
 
 // Eight elements a thread.
@@ -75,7 +97,8 @@ __global__ __launch_bounds__(256) void dequantise_mxfp4_kernel(const uint32_t *_
     Y[at] = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
 }
 
-// Large products.  A [M, K] tokens, W [O, K] channels: codes (K / 2 bytes a row) and scales (K / 32 bytes a row) as they lie.
+// Large products.  A [M, K] tokens, by steps (see above); W [O, K] channels, by steps (by_steps) or as they lie: a few tiles of tokens
+// do not pay for the turn.
 // Workgroup tile 64 TM tokens x 64 TN channels, four waves as 2 x 2.  Steps of 128 elements: 64 bytes and one dword of scales of
 // every row, copied straight to LDS, four stages, copies three steps ahead.  In LDS the 16-byte piece c of row r is at position
 // c ^ (r / 4 % 4): sixteen rows' reads of one piece meet all banks once.  A step has two parts of 64 elements (one matrix instruction
@@ -85,8 +108,8 @@ __global__ __launch_bounds__(256) void dequantise_mxfp4_kernel(const uint32_t *_
 // D[channel][token] (W is the first operand): a lane's four consecutive registers are consecutive channels.
 template <int TM, int TN>
 __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void mxfp4_gemm_kernel(const uint8_t *__restrict__ A, const uint8_t *__restrict__ As, const uint8_t *__restrict__ W,
-                                                            const uint8_t *__restrict__ Ws, const uint16_t *__restrict__ bias, int M, int O, int K,
-                                                            int n_ot, int total, uint16_t *__restrict__ Y)
+                                                            const uint8_t *__restrict__ Ws, int by_steps, const uint16_t *__restrict__ bias, int M, int O,
+                                                            int K, int n_ot, int total, uint16_t *__restrict__ Y)
 {
     constexpr int BM = 64 * TM, BN = 64 * TN, kRows = BM + BN, kStage = kRows * 68, kStages = 4;      // codes of all rows, tokens first, then their scales
     constexpr int kCodes = kRows / 64, kScales = (kRows / 64 + 3) / 4, kCopies = kCodes + kScales;       // copies a wave makes in a step: of 1 KB, of 256 bytes
@@ -102,26 +125,35 @@ __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void mxfp4_gemm_kernel(const 
 
     // copy x of wave w: sixteen rows' pieces from row 16 (w kCodes + x) of the stage on, or the scales of 64 rows; rows past the end repeat
     // the last one: their results are not stored
+    const int steps = K / 128;
     const uint8_t *pc[kCodes], *ps[kScales];
     uint32_t vc[kCodes], vs[kScales];
+    const int w_row = by_steps ? 64 : K / 2, w_step = by_steps ? 1024 : 64, ws_row = by_steps ? 4 : K / 32, ws_step = by_steps ? 4 * O : 4;
     auto clamped = [&](int r) { return r < BM ? min(r, M - 1 - i0) : min(r - BM, O - 1 - o0); };       // row of the tile's tokens or channels
 #pragma unroll
     for (int x = 0; x < kCodes; ++x) {
-        const int first = (wave * kCodes + x) * 16, r = first + (lane >> 2);                             // uniform: sixteen rows are of one matrix
-        pc[x] = first < BM ? A + (size_t)i0 * (K / 2) : W + (size_t)o0 * (K / 2);
-        vc[x] = (uint32_t)clamped(r) * (uint32_t)(K / 2) + (((lane & 3) ^ (r >> 2)) & 3) * 16;
+        const int first = (wave * kCodes + x) * 16, r = first + (lane >> 2), at = clamped(r);            // uniform: sixteen rows are of one matrix
+        pc[x] = first < BM ? A + (size_t)i0 * (K / 2) : W + (size_t)o0 * (K / 2);                        // sixteen rows are 1024 steps bytes in either order
+        vc[x] = (uint32_t)(at >> 4) * 1024u * (uint32_t)steps + (uint32_t)(at & 15) * (uint32_t)(first < BM ? 64 : w_row) + (((lane & 3) ^ (r >> 2)) & 3) * 16;
     }
+    int ks = item % steps;                           // step that the next copies bring: tiles that share rows start at steps of their own
+    auto advance = [&] { ks = ks + 1 == steps ? 0 : ks + 1; };
     int sr[kScales];                                                                                     // first row of a copy of scales (64 x 1 tiles: two waves make the same)
 #pragma unroll
     for (int x = 0; x < kScales; ++x) {
         sr[x] = min(wave * kScales + x, kRows / 64 - 1) * 64;
-        ps[x] = sr[x] < BM ? As + (size_t)i0 * (K / 32) : Ws + (size_t)o0 * (K / 32);
-        vs[x] = (uint32_t)clamped(sr[x] + lane) * (uint32_t)(K / 32);
+        ps[x] = sr[x] < BM ? As + (size_t)i0 * 4 : Ws + (size_t)o0 * ws_row;
+        vs[x] = (uint32_t)clamped(sr[x] + lane) * (uint32_t)(sr[x] < BM ? 4 : ws_row);
     }
     auto copy_one = [&](int s, int x) {
         const uint32_t to = lds_base + (s & (kStages - 1)) * kStage;
-        if (x < kCodes) copy_1k_to_lds(pc[x] + (size_t)s * 64, vc[x], to + (wave * kCodes + x) * 1024);
-        else copy_256_to_lds(ps[x - kCodes] + (size_t)s * 4, vs[x - kCodes], to + kRows * 64 + sr[x - kCodes] * 4);
+        if (x < kCodes) {
+            const int id = wave * kCodes + x;
+            copy_1k_to_lds(pc[x] + (size_t)ks * (id * 16 < BM ? 1024 : w_step), vc[x], to + id * 1024);
+        } else {
+            const int r = sr[x - kCodes];
+            copy_256_to_lds(ps[x - kCodes] + (size_t)ks * (r < BM ? 4 * M : ws_step), vs[x - kCodes], to + kRows * 64 + r * 4);
+        }
     };
 
     f32x16 acc[TN][TM];
@@ -163,7 +195,6 @@ __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void mxfp4_gemm_kernel(const 
     using Two = std::integral_constant<int, 2>;
     using Yes = std::true_type;
     using No = std::false_type;
-    const int steps = K / 128;
     // AHEAD: later steps than the next one whose copies may still be under way
     auto step = [&](int s, auto copies, auto ahead, auto last) {
         constexpr bool kCopy = decltype(copies)::value, kLast = decltype(last)::value;
@@ -171,6 +202,7 @@ __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void mxfp4_gemm_kernel(const 
             spread(i, kOps, [&](int x) { read_op(1, s, 1, x); });
             if constexpr (kCopy) spread(i, kCopies, [&](int x) { copy_one(s + 3, x); });
         });
+        if constexpr (kCopy) advance();
         if constexpr (!kLast) {
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(ahead)::value * kCopies) : "memory");
             lds_barrier();
@@ -187,9 +219,11 @@ __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void mxfp4_gemm_kernel(const 
         }
     };
 
-    for (int s = 0; s < min(steps, 3); ++s)
+    for (int s = 0; s < min(steps, 3); ++s) {
 #pragma unroll
         for (int x = 0; x < kCopies; ++x) copy_one(s, x);
+        advance();
+    }
     if (steps > 2)       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kCopies) : "memory");
     else if (steps == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kCopies) : "memory");
     else                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -205,33 +239,22 @@ __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void mxfp4_gemm_kernel(const 
     if (s + 1 < steps) step(s++, No{}, Part0{}, No{});
     step(s, No{}, Part0{}, Yes{});
 
-    // register 4q + r of acc[a][b], lane (l32, g): channel 32 a + 8 q + 4 g + r, token 32 b + l32; v_permlane32_swap brings the
-    // two halves of a 16-byte store together
-    auto swap32 = [](uint32_t &lo, uint32_t &hi) {
-        const auto r = __builtin_amdgcn_permlane32_swap(lo, hi, false, false);
-        lo = r[0];
-        hi = r[1];
-    };
+    // register 4q + r of acc[a][b], lane (l32, g): channel 32 a + 8 q + 4 g + r, token 32 b + l32
+    lds_barrier();                                   // everybody has read the last stage
+    const int ch0 = o0 + wo, tok0 = i0 + wi;
+    float bi[TN][4][4];
 #pragma unroll
     for (int a = 0; a < TN; ++a)
 #pragma unroll
-        for (int q = 0; q < 4; q += 2) {
-            float bi[2][4];
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) bi[h][r] = bias ? bf16_bits_to_f32(bias[min(o0 + wo + 32 * a + 8 * (q + h) + 4 * g + r, O - 1)]) : 0.f;
-#pragma unroll
-            for (int b = 0; b < TM; ++b) {
-                const int i = i0 + wi + 32 * b + l32, o = o0 + wo + 32 * a + 8 * q + 8 * g;
-                const f32x16 &v = acc[a][b];
-                uint32_t x0 = pack_bf16(v[4 * q] + bi[0][0], v[4 * q + 1] + bi[0][1]), y0 = pack_bf16(v[4 * q + 2] + bi[0][2], v[4 * q + 3] + bi[0][3]);
-                uint32_t x1 = pack_bf16(v[4 * q + 4] + bi[1][0], v[4 * q + 5] + bi[1][1]), y1 = pack_bf16(v[4 * q + 6] + bi[1][2], v[4 * q + 7] + bi[1][3]);
-                swap32(x0, x1);
-                swap32(y0, y1);
-                if (i < M && o < O) *(uint4 *)(Y + (size_t)i * O + o) = make_uint4(x0, y0, x1, y1);      // O is a multiple of 8
-            }
+        for (int q = 0; q < 4; ++q) {
+            const int o = min(ch0 + 32 * a + 8 * q + 4 * g, O - 4);
+            const uint2 u = bias ? *(const uint2 *)(bias + o) : make_uint2(0, 0);
+            bi[a][q][0] = bf16_lo(u.x); bi[a][q][1] = bf16_hi(u.x); bi[a][q][2] = bf16_lo(u.y); bi[a][q][3] = bf16_hi(u.y);
         }
+    store_tile<TM, TN>(smem + wave * kStoreBytes<TN>, [&](int a, int b, int q, float (&v)[4]) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = acc[a][b][4 * q + r] + bi[a][q][r];
+    }, lane, M - tok0, O - ch0, Y + (size_t)tok0 * O + ch0, (size_t)O);
 }
 
 // Few tokens (at most 16 T): one launch, bound by the weights' bytes and by latency.  A wave takes 16 channels and a part of K
@@ -295,7 +318,16 @@ hipError_t launch_quantise_mxfp4(const void *X, long rows, int cols, void *codes
 {
     const long pieces = rows * (cols / 8), grid = (pieces + 255) / 256;
     if (grid > 0x7FFFFFFFL) return hipErrorInvalidValue;
-    quantise_mxfp4_kernel<<<(unsigned)grid, 256, 0, st>>>((const uint4 *)X, pieces, (uint32_t *)codes, (uint8_t *)scales);
+    quantise_mxfp4_kernel<false><<<(unsigned)grid, 256, 0, st>>>((const uint4 *)X, pieces, (uint32_t *)codes, (uint8_t *)scales, 0, 0, WeightsIn{});
+    return hipGetLastError();
+}
+
+hipError_t launch_mxfp4_operands(const void *X, int M, int K, void *codes, void *scales, const void *W, const void *Ws, int O, void *W_out, void *Ws_out, hipStream_t st)
+{
+    const long pieces = (long)M * (K / 8), first_w = (pieces + 255) / 256, grid = first_w + (W_out ? ((long)O * (K / 32) + 255) / 256 : 0);
+    if (grid > 0x7FFFFFFFL) return hipErrorInvalidValue;
+    const WeightsIn w = {(const i32x4 *)W, (const uint32_t *)Ws, (i32x4 *)W_out, (uint32_t *)Ws_out, O, (unsigned)first_w};
+    quantise_mxfp4_kernel<true><<<(unsigned)grid, 256, 0, st>>>((const uint4 *)X, pieces, (uint32_t *)codes, (uint8_t *)scales, M, K / 128, w);
     return hipGetLastError();
 }
 
@@ -320,12 +352,12 @@ template <int T> hipError_t launch_few(const void *X, const void *W, const void 
     return hipGetLastError();
 }
 template <int TM, int TN>
-hipError_t launch_gemm(const void *A, const void *As, const void *W, const void *Ws, const void *bias, int M, int O, int K, void *Y, hipStream_t st)
+hipError_t launch_gemm(const void *A, const void *As, const void *W, const void *Ws, bool by_steps, const void *bias, int M, int O, int K, void *Y, hipStream_t st)
 {
     const int n_it = (M + 64 * TM - 1) / (64 * TM), n_ot = (O + 64 * TN - 1) / (64 * TN);
     const long total = (long)n_it * n_ot;
     if (total > 0x7FFFFFF0L) return hipErrorInvalidValue;
-    mxfp4_gemm_kernel<TM, TN><<<(unsigned)xcd_grid(total), 256, 0, st>>>((const uint8_t *)A, (const uint8_t *)As, (const uint8_t *)W, (const uint8_t *)Ws,
+    mxfp4_gemm_kernel<TM, TN><<<(unsigned)xcd_grid(total), 256, 0, st>>>((const uint8_t *)A, (const uint8_t *)As, (const uint8_t *)W, (const uint8_t *)Ws, by_steps,
                                                                          (const uint16_t *)bias, M, O, K, n_ot, (int)total, (uint16_t *)Y);
     return hipGetLastError();
 }
@@ -337,12 +369,14 @@ hipError_t launch_mxfp4_few(const void *X, const void *W, const void *Ws, const 
     return launch_few<2>(X, W, Ws, bias, M, O, K, Y, st);
 }
 
-hipError_t launch_mxfp4_gemm(const void *A, const void *As, const void *W, const void *Ws, const void *bias, int M, int O, int K, void *Y, hipStream_t st)
+bool mxfp4_turns_weights(int M, int O) { return M >= 2L * O; }
+
+hipError_t launch_mxfp4_gemm(const void *A, const void *As, const void *W, const void *Ws, bool by_steps, const void *bias, int M, int O, int K, void *Y, hipStream_t st)
 {
     const long wide = (long)((M + 255) / 256) * ((O + 255) / 256), n_ot = (O + 127) / 128;
-    if (wide >= 160) return launch_gemm<4, 4>(A, As, W, Ws, bias, M, O, K, Y, st);
-    if ((M + 127) / 128 * n_ot >= 400) return launch_gemm<2, 2>(A, As, W, Ws, bias, M, O, K, Y, st);
-    return launch_gemm<1, 2>(A, As, W, Ws, bias, M, O, K, Y, st);
+    if (wide >= 160) return launch_gemm<4, 4>(A, As, W, Ws, by_steps, bias, M, O, K, Y, st);
+    if ((M + 127) / 128 * n_ot >= 400) return launch_gemm<2, 2>(A, As, W, Ws, by_steps, bias, M, O, K, Y, st);
+    return launch_gemm<1, 2>(A, As, W, Ws, by_steps, bias, M, O, K, Y, st);
 }
 
 }  // namespace sla

@@ -17,7 +17,7 @@ sla_status_t check_matrix(int64_t rows, int32_t cols)
     return SLA_OK;
 }
 
-struct MxPlan { size_t off_scales, total; };
+struct MxPlan { size_t off_scales, off_w, off_ws, total; };      // codes and scales of x, those of W where they are turned
 sla_status_t make_mx_plan(int32_t N, int32_t d_in, int32_t d_out, MxPlan &mp)
 {
     if (N < 0 || d_in <= 0 || d_out <= 0) return fail(SLA_ERR_INVALID_ARG, "bad sizes (N=%d d_in=%d d_out=%d)", N, d_in, d_out);
@@ -25,8 +25,11 @@ sla_status_t make_mx_plan(int32_t N, int32_t d_in, int32_t d_out, MxPlan &mp)
     if (d_out % 8 != 0) return fail(SLA_ERR_UNSUPPORTED, "d_out = %d; only multiples of 8 are implemented", d_out);
     if ((double)N * d_in >= 4.0e9 || (double)d_out * d_in >= 4.0e9 || (double)N * d_out >= 4.0e9) return fail(SLA_ERR_UNSUPPORTED, "matrix of 4e9 elements or more");
     if (d_in > 1 << 24) return fail(SLA_ERR_UNSUPPORTED, "d_in = %d; at most 2^24 are implemented", d_in);       // 256 rows of codes within 2 GB
-    mp.off_scales = align_up((size_t)N * d_in / 2, 256);
-    mp.total = sla::mxfp4_few(N) ? 0 : mp.off_scales + align_up((size_t)N * d_in / 32, 256);
+    const bool turned = sla::mxfp4_turns_weights(N, d_out);
+    mp.off_scales = align_up((size_t)N, 16) * d_in / 2;
+    mp.off_w = mp.off_scales + align_up((size_t)N * d_in / 32, 256);
+    mp.off_ws = mp.off_w + (turned ? align_up((size_t)d_out, 16) * d_in / 2 : 0);
+    mp.total = sla::mxfp4_few(N) ? 0 : mp.off_ws + (turned ? align_up((size_t)d_out * d_in / 32, 256) : 0);
     return SLA_OK;
 }
 
@@ -78,9 +81,11 @@ sla_status_t sla_mxfp4_linear(const void *x, const void *W_codes, const void *W_
     if (!workspace) return fail(SLA_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", mp.total);
     if (!aligned(workspace, 256)) return fail(SLA_ERR_WORKSPACE, "workspace must be 256-byte aligned");
     if (workspace_bytes < mp.total) return fail(SLA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, mp.total);
+    const bool turned = sla::mxfp4_turns_weights(N, d_out);
     void *const codes = workspace, *const scales = at<void>(workspace, mp.off_scales);
-    SLA_HIP(sla::launch_quantise_mxfp4(x, N, d_in, codes, scales, st));
-    SLA_HIP(sla::launch_mxfp4_gemm(codes, scales, W_codes, W_scales, bias, N, d_out, d_in, y, st));
+    void *const W = turned ? at<void>(workspace, mp.off_w) : nullptr, *const Ws = at<void>(workspace, mp.off_ws);
+    SLA_HIP(sla::launch_mxfp4_operands(x, N, d_in, codes, scales, W_codes, W_scales, d_out, W, Ws, st));
+    SLA_HIP(sla::launch_mxfp4_gemm(codes, scales, turned ? W : W_codes, turned ? Ws : W_scales, turned, bias, N, d_out, d_in, y, st));
     return SLA_OK;
 }
 

@@ -103,8 +103,12 @@ hipError_t launch_restore_rows(const void *codes, const float *scales, long rows
 // Microscaled 4-bit numbers (k_mxfp4.hip): codes rows x cols / 2 bytes and scales rows x cols / 32 bytes, cols a multiple of 32
 hipError_t launch_quantise_mxfp4(const void *X, long rows, int cols, void *codes, void *scales, hipStream_t st);
 hipError_t launch_dequantise_mxfp4(const void *codes, const void *scales, long rows, int cols, void *Y, hipStream_t st);
-// Y bf16 [M,O] = A [M,K] W [O,K]^T + bias of two matrices in that form, K a multiple of 128, O of 8; bias may be NULL
-hipError_t launch_mxfp4_gemm(const void *A, const void *As, const void *W, const void *Ws, const void *bias, int M, int O, int K, void *Y, hipStream_t st);
+// X bf16 [M,K], K a multiple of 128 -> codes (M rounded up to 16 rows) and scales in the product's order, by steps (k_mxfp4.hip); with
+// W_out != NULL also W, Ws (O rows as above) -> W_out (O rounded up to 16 rows), Ws_out in that order
+hipError_t launch_mxfp4_operands(const void *X, int M, int K, void *codes, void *scales, const void *W, const void *Ws, int O, void *W_out, void *Ws_out, hipStream_t st);
+bool mxfp4_turns_weights(int M, int O);            // whether a product with M tokens takes its weights by steps
+// Y bf16 [M,O] = A [M,K] W [O,K]^T + bias: A, As by steps, W, Ws by steps or as they lie, K a multiple of 128, O of 8; bias may be NULL
+hipError_t launch_mxfp4_gemm(const void *A, const void *As, const void *W, const void *Ws, bool by_steps, const void *bias, int M, int O, int K, void *Y, hipStream_t st);
 // the same for few rows of bf16 X, quantised on the way (no workspace)
 bool mxfp4_few(int M);
 hipError_t launch_mxfp4_few(const void *X, const void *W, const void *Ws, const void *bias, int M, int O, int K, void *Y, hipStream_t st);
