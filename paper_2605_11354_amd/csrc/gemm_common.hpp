@@ -4,6 +4,15 @@
 
 namespace sla {
 
+// two copies of 1 KB as copy_1k_to_lds makes them, the second 1 KB behind the first in LDS: four scalar instructions less
+__device__ __forceinline__ void copy_2k_to_lds(const uint8_t *base, uint32_t voff0, uint32_t voff1, uint32_t lds_addr)
+{
+    uint32_t saved_m0;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
+                 "global_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+                 : "=&s"(saved_m0) : "v"(voff0), "v"(voff1), "s"(base), "s"(lds_addr) : "memory", "scc");
+}
+
 // 256 bytes global -> LDS: lane l moves the dword at base + voff(l) to LDS byte lds_addr + 4 l (otherwise as copy_1k_to_lds)
 __device__ __forceinline__ void copy_256_to_lds(const uint8_t *base, uint32_t voff, uint32_t lds_addr)
 {

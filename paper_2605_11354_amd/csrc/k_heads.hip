@@ -178,13 +178,13 @@ __device__ __forceinline__ Item item_of(const HeadsArgs &a, int item)
 template <class T> __device__ __forceinline__ T pick(T const (&p)[3], int tensor) { return tensor == 0 ? p[0] : tensor == 1 ? p[1] : p[2]; }
 }  // namespace
 
-// bf16 outputs.  A unit is TOK tokens of 64 / TOK neighbouring items: where tokens are few, a workgroup takes few of them and all the
+// bf16 outputs.  A unit is TOK tokens of 8 ROWS / TOK neighbouring items, ROWS rows a lane: where tokens are few, a workgroup takes few of them and all the
 // heads rather than many tokens of few heads, for which it would compute as many angles.  The rows of the next unit are asked
 // for before this one's are stored: a load behind a store would wait for it.
-template <int ROT, int TOK>
+template <int ROT, int TOK, int ROWS>
 __global__ __launch_bounds__(256, 4) void heads_kernel(HeadsArgs a)
 {
-    constexpr int kOct = TOK / 8, kItems = 64 / TOK;
+    constexpr int kOct = TOK / 8, kItems = ROWS / kOct;
     __shared__ long in_off[TOK], out_off[TOK];
     __shared__ int pos_row[TOK];
     __shared__ __attribute__((aligned(16))) float table[ROT ? TOK * kCsPitch<true> : 4];
@@ -194,10 +194,10 @@ __global__ __launch_bounds__(256, 4) void heads_kernel(HeadsArgs a)
     const int valid = (int)min((long)TOK, (long)a.B * a.N - first);
     lay_out_tokens<TOK, false>(a, 0, first, valid, in_off, out_off, pos_row);
     const int i0 = (int)part * a.chunk, i1 = min(i0 + a.chunk, a.tensors * a.H);
-    uint4 rows[8], nxt[8];
+    uint4 rows[ROWS], nxt[ROWS];
     auto load = [&](int unit) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+        for (int k = 0; k < ROWS; ++k)
             if (8 * (k % kOct) < valid && unit + k / kOct < i1) {
                 const Item it = item_of(a, unit + k / kOct);
                 nxt[k] = *(const uint4 *)(pick(a.x, it.tensor) + it.head * a.hs + 8 * o + in_off[r0 + 8 * (k % kOct)]);
@@ -209,11 +209,11 @@ __global__ __launch_bounds__(256, 4) void heads_kernel(HeadsArgs a)
     int have = -1;                                   // tensor whose weights these are
     for (int unit = i0 + wave * kItems; unit < i1; unit += 4 * kItems) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) rows[k] = nxt[k];
+        for (int k = 0; k < ROWS; ++k) rows[k] = nxt[k];
         load(unit + 4 * kItems);
         Item it;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < ROWS; ++k) {
             if (unit + k / kOct >= i1) break;
             const int r = r0 + 8 * (k % kOct);
             if (k % kOct == 0) {
@@ -501,16 +501,19 @@ long token_blocks(const HeadsArgs &a, int tok) { return ((long)a.B * a.N + tok -
 
 template <int ROT> hipError_t launch_heads_rot(HeadsArgs a, int bq, hipStream_t st)
 {
-    const bool few = few_tokens(a);
+    // units of two rows a lane instead of eight where even those make few workgroups: one after the other in a wave they are latency
+    // (32 tokens of 16 heads: 8.3 us and 5.9)
+    const bool few = few_tokens(a), least = few && token_blocks(a, 16) * a.tensors * a.H <= 4 * 512;
     const int tok = bq ? bq : few ? 16 : 64;
     const long blocks = bq ? (long)a.B * ((a.N + tok - 1) / tok) : token_blocks(a, tok);
-    split_items(a, blocks, bq == 128 ? 2 : bq || !few ? 4 : 16, bq != 0);
+    split_items(a, blocks, bq == 128 ? 2 : bq || !few || least ? 4 : 16, bq != 0);
     const long grid = blocks * a.splits;
     if (grid > 0x7FFFFFFFL) return hipErrorInvalidValue;
     if (bq == 64)       heads_e4m3_kernel<ROT, 1><<<(unsigned)grid, 256, 0, st>>>(a);
     else if (bq == 128) heads_e4m3_kernel<ROT, 2><<<(unsigned)grid, 256, 0, st>>>(a);
-    else if (few)       heads_kernel<ROT, 16><<<(unsigned)grid, 256, 0, st>>>(a);
-    else                heads_kernel<ROT, 64><<<(unsigned)grid, 256, 0, st>>>(a);
+    else if (least)     heads_kernel<ROT, 16, 2><<<(unsigned)grid, 256, 0, st>>>(a);
+    else if (few)       heads_kernel<ROT, 16, 8><<<(unsigned)grid, 256, 0, st>>>(a);
+    else                heads_kernel<ROT, 64, 8><<<(unsigned)grid, 256, 0, st>>>(a);
     return hipGetLastError();
 }
 // the plan of a gradient's launch: tokens of a workgroup, and the slots of its partial sums

@@ -112,7 +112,8 @@ __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void mxfp4_gemm_kernel(const 
                                                             int K, int n_ot, int total, uint16_t *__restrict__ Y)
 {
     constexpr int BM = 64 * TM, BN = 64 * TN, kRows = BM + BN, kStage = kRows * 68, kStages = 4;      // codes of all rows, tokens first, then their scales
-    constexpr int kCodes = kRows / 64, kScales = (kRows / 64 + 3) / 4, kCopies = kCodes + kScales;       // copies a wave makes in a step: of 1 KB, of 256 bytes
+    constexpr int kScales = (kRows / 64 + 3) / 4, kCopies = TM + TN + kScales;   // copies a wave makes in a step: of 1 KB (A, W), of 256 bytes
+    constexpr int kOpsA = (TM + 1) / 2, kOpsW = TN / 2, kCopyOps = kOpsA + kOpsW + kScales;       // in pairs
     __shared__ __attribute__((aligned(1024))) uint8_t smem[kStages * kStage];
     const int item = (int)xcd_remap(blockIdx.x, total);
     if (item >= total) return;
@@ -123,36 +124,51 @@ __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void mxfp4_gemm_kernel(const 
     const int wi = (wave & 1) * 32 * TM, wo = (wave >> 1) * 32 * TN;
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
 
-    // copy x of wave w: sixteen rows' pieces from row 16 (w kCodes + x) of the stage on, or the scales of 64 rows; rows past the end repeat
-    // the last one: their results are not stored
+    // copies of wave w: sixteen rows' pieces each of tokens from row 16 TM w of the tile on and of channels from row 16 TN w on, the scales
+    // of 64 rows from row 64 kScales w of both on; rows past the end repeat the last one: their results are not stored
     const int steps = K / 128;
-    const uint8_t *pc[kCodes], *ps[kScales];
-    uint32_t vc[kCodes], vs[kScales];
-    const int w_row = by_steps ? 64 : K / 2, w_step = by_steps ? 1024 : 64, ws_row = by_steps ? 4 : K / 32, ws_step = by_steps ? 4 * O : 4;
-    auto clamped = [&](int r) { return r < BM ? min(r, M - 1 - i0) : min(r - BM, O - 1 - o0); };       // row of the tile's tokens or channels
+    const int w_row = by_steps ? 64 : K / 2, ws_row = by_steps ? 4 : K / 32;
+    const size_t w_step = by_steps ? 1024 : 64, ws_step = by_steps ? 4 * (size_t)O : 4;
+    uint32_t va[TM], vw[TN], vs[kScales];
+    auto place = [&](int r, int last, int row_bytes) {                           // of the lane's piece; sixteen rows are 1024 steps bytes in either order
+        const int at = min(r, last);
+        return (uint32_t)(at >> 4) * 1024u * (uint32_t)steps + (uint32_t)(at & 15) * (uint32_t)row_bytes + (((lane & 3) ^ (r >> 2)) & 3) * 16;
+    };
 #pragma unroll
-    for (int x = 0; x < kCodes; ++x) {
-        const int first = (wave * kCodes + x) * 16, r = first + (lane >> 2), at = clamped(r);            // uniform: sixteen rows are of one matrix
-        pc[x] = first < BM ? A + (size_t)i0 * (K / 2) : W + (size_t)o0 * (K / 2);                        // sixteen rows are 1024 steps bytes in either order
-        vc[x] = (uint32_t)(at >> 4) * 1024u * (uint32_t)steps + (uint32_t)(at & 15) * (uint32_t)(first < BM ? 64 : w_row) + (((lane & 3) ^ (r >> 2)) & 3) * 16;
-    }
+    for (int x = 0; x < TM; ++x) va[x] = place((wave * TM + x) * 16 + (lane >> 2), M - 1 - i0, 64);
+#pragma unroll
+    for (int x = 0; x < TN; ++x) vw[x] = place((wave * TN + x) * 16 + (lane >> 2), O - 1 - o0, w_row);
     int ks = item % steps;                           // step that the next copies bring: tiles that share rows start at steps of their own
-    auto advance = [&] { ks = ks + 1 == steps ? 0 : ks + 1; };
-    int sr[kScales];                                                                                     // first row of a copy of scales (64 x 1 tiles: two waves make the same)
+    const uint8_t *ba, *bw, *bs[kScales];            // where that step begins
+    const uint8_t *const a0 = A + (size_t)i0 * (K / 2), *const w0 = W + (size_t)o0 * (K / 2), *s0[kScales];
+    size_t s_step[kScales];
+    int sr[kScales];                                 // first row of a copy of scales (64 x 128 tiles: two waves make the same)
 #pragma unroll
     for (int x = 0; x < kScales; ++x) {
         sr[x] = min(wave * kScales + x, kRows / 64 - 1) * 64;
-        ps[x] = sr[x] < BM ? As + (size_t)i0 * 4 : Ws + (size_t)o0 * ws_row;
-        vs[x] = (uint32_t)clamped(sr[x] + lane) * (uint32_t)(sr[x] < BM ? 4 : ws_row);
+        const bool tokens = sr[x] < BM;
+        s0[x] = tokens ? As + (size_t)i0 * 4 : Ws + (size_t)o0 * ws_row;
+        s_step[x] = tokens ? 4 * (size_t)M : ws_step;
+        vs[x] = (uint32_t)min((tokens ? sr[x] : sr[x] - BM) + lane, (tokens ? M - i0 : O - o0) - 1) * (uint32_t)(tokens ? 4 : ws_row);
     }
+    auto aim = [&] {
+        ba = a0 + (size_t)ks * 1024;
+        bw = w0 + ks * w_step;
+#pragma unroll
+        for (int x = 0; x < kScales; ++x) bs[x] = s0[x] + ks * s_step[x];
+        ks = ks + 1 == steps ? 0 : ks + 1;
+    };
     auto copy_one = [&](int s, int x) {
         const uint32_t to = lds_base + (s & (kStages - 1)) * kStage;
-        if (x < kCodes) {
-            const int id = wave * kCodes + x;
-            copy_1k_to_lds(pc[x] + (size_t)ks * (id * 16 < BM ? 1024 : w_step), vc[x], to + id * 1024);
+        if (x < kOpsA) {
+            if constexpr (TM == 1) copy_1k_to_lds(ba, va[0], to + wave * 1024);
+            else copy_2k_to_lds(ba, va[2 * x], va[2 * x + 1], to + (wave * TM + 2 * x) * 1024);
+        } else if (x < kOpsA + kOpsW) {
+            const int p = x - kOpsA;
+            copy_2k_to_lds(bw, vw[2 * p], vw[2 * p + 1], to + BM * 64 + (wave * TN + 2 * p) * 1024);
         } else {
-            const int r = sr[x - kCodes];
-            copy_256_to_lds(ps[x - kCodes] + (size_t)ks * (r < BM ? 4 * M : ws_step), vs[x - kCodes], to + kRows * 64 + r * 4);
+            const int p = x - kOpsA - kOpsW;
+            copy_256_to_lds(bs[p], vs[p], to + kRows * 64 + sr[p] * 4);
         }
     };
 
@@ -166,11 +182,14 @@ __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void mxfp4_gemm_kernel(const 
     constexpr int kOps = TM + TN;                                                // operands of a part: TN of W, then TM of x
     i32x4 op[2][kOps];
     int sc[kOps], next_sc[kOps];
-    auto row_of = [&](int x) { return (x < TN ? BM + wo + 32 * x : wi + 32 * (x - TN)) + l32; };
-    auto read_op = [&](int set, int s, int t, int x) {
-        op[set][x] = *(const i32x4 *)(smem + (s & (kStages - 1)) * kStage + row_of(x) * 64 + (((2 * t + g) ^ (l32 >> 2)) & 3) * 16);
+    // LDS bytes of the lane's piece of operand 0 of W and of x in part 0 and 1, and of their scales; other operands are 32 rows on
+    const uint32_t row_w = BM + wo + l32, row_x = wi + l32, piece0 = ((g ^ (l32 >> 2)) & 3) * 16, piece1 = (((2 + g) ^ (l32 >> 2)) & 3) * 16;
+    const uint32_t at_w[2] = {row_w * 64 + piece0, row_w * 64 + piece1}, at_x[2] = {row_x * 64 + piece0, row_x * 64 + piece1};
+    const uint32_t at_sw = kRows * 64 + row_w * 4, at_sx = kRows * 64 + row_x * 4;
+    auto read_op = [&](int set, uint32_t stage, int t, int x) {
+        op[set][x] = *(const i32x4 *)(x < TN ? smem + (stage + at_w[t]) + x * 2048 : smem + (stage + at_x[t]) + (x - TN) * 2048);
     };
-    auto read_scale = [&](int s, int x) { return *(const int *)(smem + (s & (kStages - 1)) * kStage + kRows * 64 + row_of(x) * 4); };
+    auto read_scale = [&](uint32_t stage, int x) { return *(const int *)(x < TN ? smem + (stage + at_sw) + x * 128 : smem + (stage + at_sx) + (x - TN) * 128); };
     auto mine = [&](int dword) { return (int)((uint32_t)dword >> (8 * g)); };    // this half's two blocks of the step: bytes 0 and 2
     auto wide = [](i32x4 u) { return i32x8{u[0], u[1], u[2], u[3], 0, 0, 0, 0}; };
     // the products of a part; what `between` does is spread over the gaps behind them
@@ -198,19 +217,20 @@ __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void mxfp4_gemm_kernel(const 
     // AHEAD: later steps than the next one whose copies may still be under way
     auto step = [&](int s, auto copies, auto ahead, auto last) {
         constexpr bool kCopy = decltype(copies)::value, kLast = decltype(last)::value;
+        const uint32_t stage = (s & (kStages - 1)) * kStage, next = ((s + 1) & (kStages - 1)) * kStage;
+        if constexpr (kCopy) aim();
         multiply(Part0{}, [&](int i) {
-            spread(i, kOps, [&](int x) { read_op(1, s, 1, x); });
-            if constexpr (kCopy) spread(i, kCopies, [&](int x) { copy_one(s + 3, x); });
+            spread(i, kOps, [&](int x) { read_op(1, stage, 1, x); });
+            if constexpr (kCopy) spread(i, kCopyOps, [&](int x) { copy_one(s + 3, x); });
         });
-        if constexpr (kCopy) advance();
         if constexpr (!kLast) {
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(ahead)::value * kCopies) : "memory");
             lds_barrier();
         }
         multiply(Part1{}, [&](int i) {
             if constexpr (!kLast) {
-                spread(i, kOps, [&](int x) { read_op(0, s + 1, 0, x); });
-                spread(i, kOps, [&](int x) { next_sc[x] = read_scale(s + 1, x); });
+                spread(i, kOps, [&](int x) { read_op(0, next, 0, x); });
+                spread(i, kOps, [&](int x) { next_sc[x] = read_scale(next, x); });
             }
         });
         if constexpr (!kLast) {
@@ -220,9 +240,9 @@ __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void mxfp4_gemm_kernel(const 
     };
 
     for (int s = 0; s < min(steps, 3); ++s) {
+        aim();
 #pragma unroll
-        for (int x = 0; x < kCopies; ++x) copy_one(s, x);
-        advance();
+        for (int x = 0; x < kCopyOps; ++x) copy_one(s, x);
     }
     if (steps > 2)       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kCopies) : "memory");
     else if (steps == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kCopies) : "memory");
