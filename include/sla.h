@@ -203,13 +203,16 @@ sla_status_t sla_fp8_linear_qkv(const void *x, const void *W, const void *bias, 
                                 void *workspace, size_t workspace_bytes, void *stream);
 
 /*
- * Training of that layer (Alg. 2; straight through both quantisers) with its input kept in 8 bits.  sla_fp8_linear_save is
- * sla_fp8_linear (the same y, bit for bit) that leaves the E4M3 codes and the scales of x, which it multiplies anyway, in
- * `checkpoint`: sla_fp8_checkpoint_bytes(N, d_in), about N (d_in + 4) bytes, half of x; x itself is not needed again.
+ * Training of that layer (Alg. 2; straight through both quantisers) with its input kept in 8 bits.  sla_fp8_linear_save computes
+ * y as sla_fp8_linear does and leaves the E4M3 codes and the scales of x, which it multiplies anyway, in `checkpoint`:
+ * sla_fp8_checkpoint_bytes(N, d_in), about N (d_in + 4) bytes, half of x; x itself is not needed again.  Its scales are
+ * max(amax, 1e-8) * fp32(1 / 448), what PyTorch on the GPU makes of the formula amax / 448.0, so that its codes are those of the
+ * fake-quantised layer as one writes it there; sla_fp8_linear divides: where x / scale lies half-way between two codes, the two can
+ * choose different ones.
  * sla_fp8_linear_grad takes them for the gradients
  *     dx = dy W_q     dW = dy^T x_q     db = sum over tokens of dy        x_q, W_q = bf16(code * scale)
  * with products summed in fp32 in a fixed order (no atomics: the same inputs give the same bits) and rounded once to bf16.
- *   x, W, bias, y   as sla_fp8_linear; W in sla_fp8_linear_grad is that of the forward (quantised again; needed for dx only)
+ *   x, W, bias, y   of the sizes and types of sla_fp8_linear; W in sla_fp8_linear_grad is that of the forward (quantised again; needed for dx only)
  *   dy    in   bf16 [N, d_out]
  *   dx    out  bf16 [N, d_in] or NULL;   dW  out  bf16 [d_out, d_in] or NULL;   db  out  bf16 [d_out] or NULL (only with dW)
  *   workspace  sla_fp8_linear_grad_workspace_bytes(N, d_in, d_out) bytes for both calls, 256-byte aligned as the checkpoint;

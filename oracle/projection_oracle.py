@@ -72,10 +72,19 @@ def heads_backward(x, norm, w, eps, axes, pairing, base, pos, dy, per_head=False
 
 # ---- the FP8 layer's gradients
 def e4m3_rows(bits):
-    """(values, scales) of bf16 rows as the layer quantises them: E4M3 numbers, one fp32 scale per row."""
-    codes, scales = sla_oracle.quantise_e4m3_rows(bits)
-    grid = sla_oracle._e4m3_grid()
-    return np.where(codes & 0x80, -1.0, 1.0) * grid[(codes & 0x7F).astype(np.int64)], scales.astype(np.float64)
+    """(values, scales) of bf16 rows as the layer's training form quantises them: E4M3 numbers of fp32 quotients, one fp32 scale per
+    row, max(amax, 1e-8) times the fp32 number 1/448."""
+    x = (np.ascontiguousarray(bits, np.uint16).astype(np.uint32) << 16).view(np.float32)
+    scales = np.maximum(np.abs(x).max(-1), np.float32(1e-8)) * (np.float32(1) / np.float32(448))
+    assert scales.dtype == np.float32
+    codes = sla_oracle._e4m3_cast(np.clip(x / scales[:, None], np.float32(-448), np.float32(448)))
+    return np.where(codes & 0x80, -1.0, 1.0) * sla_oracle._e4m3_grid()[(codes & 0x7F).astype(np.int64)], scales.astype(np.float64)
+
+
+def fp8_linear_train(x_bits, W_bits, bias_bits):
+    """y of the training form in exact products."""
+    (xc, xs), (wc, ws) = e4m3_rows(x_bits), e4m3_rows(W_bits)
+    return (xc * xs[:, None]) @ (wc * ws[:, None]).T + bf16_to_f64(bias_bits)
 
 
 def fp8_linear_backward(x_bits, W_bits, dy):

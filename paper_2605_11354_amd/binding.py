@@ -374,7 +374,7 @@ def sla_fp8_linear_grad_workspace_bytes(N, d_in, d_out) -> int:
 
 
 def sla_fp8_linear_save(x, W, bias, y, checkpoint, workspace=None):
-    """sla_fp8_linear that leaves x in 8 bits in `checkpoint` (uint8, sla_fp8_checkpoint_bytes(N, d_in) long)."""
+    """The FP8 layer's training form: y, and x in 8 bits in `checkpoint` (uint8, sla_fp8_checkpoint_bytes(N, d_in) long)."""
     (N, d_in), d_out, bf, dev = x.shape, W.shape[0], torch.bfloat16, _device()
     if workspace is None:
         workspace = _scratch(sla_fp8_linear_grad_workspace_bytes(N, d_in, d_out), x.device)

@@ -40,7 +40,8 @@ struct RowsIn {
 // The first half groups belong to matrix a, the others to b: the few rows of the weights would be a launch of their own,
 // most of which is waiting.  Measured: 43968 + 3072 rows of 1024 in 25 us = 5.5 TB/s (two launches, a row per wave read twice, with
 // the division's expansion: 32 + 5.3 us); 1374 + 3072 rows 8.6 us (4.3 + 7.3 us and the gap between them).
-template <int SL, bool ONE>                          // slices per wave and pass; rows of one pass
+// TRAINING: scales as training_scale() has them.
+template <int SL, bool ONE, bool TRAINING>           // slices per wave and pass; rows of one pass
 __global__ __launch_bounds__(256) void quantise_rows_kernel(RowsIn ma, RowsIn mb, int cols)
 {
     asm volatile("" ::"s"(ma.X), "s"(ma.rows), "s"(ma.codes), "s"(ma.scales), "s"(mb.X), "s"(mb.rows), "s"(mb.codes), "s"(mb.scales), "s"(cols));      // all kernel arguments in one batch of scalar loads, here
@@ -75,7 +76,8 @@ __global__ __launch_bounds__(256) void quantise_rows_kernel(RowsIn ma, RowsIn mb
     amax = fmaxf(amax, __shfl_xor(amax, 2, 64));
     if (c == 0) red[wave][r0] = amax;
     __syncthreads();
-    const float scale = fmaxf(fmaxf(fmaxf(red[0][r0], red[1][r0]), fmaxf(red[2][r0], red[3][r0])), 1e-8f) / 448.0f;
+    const float top = fmaxf(fmaxf(red[0][r0], red[1][r0]), fmaxf(red[2][r0], red[3][r0]));
+    const float scale = TRAINING ? training_scale(top) : fmaxf(top, 1e-8f) / 448.0f;
     if (wave == 0 && c == 0 && row < R) m.scales[32 * grp + row] = scale;
     uint8_t *const out = m.codes + 32 * grp * cols + (((c & 1) * 2 + (c >> 1)) * R + row) * 16;
     const BlockDivisor divide(scale);
@@ -89,15 +91,22 @@ __global__ __launch_bounds__(256) void quantise_rows_kernel(RowsIn ma, RowsIn mb
     }
 }
 
+namespace {
+template <bool TRAINING> hipError_t launch_rows(const RowsIn &a, const RowsIn &b, int cols, hipStream_t st)
+{
+    const unsigned grid = (unsigned)(2 * ((a.rows + 31) / 32 + (b.rows + 31) / 32));
+    if (cols <= 1024)      quantise_rows_kernel<4, true, TRAINING><<<grid, 256, 0, st>>>(a, b, cols);
+    else if (cols <= 2048) quantise_rows_kernel<8, true, TRAINING><<<grid, 256, 0, st>>>(a, b, cols);
+    else                   quantise_rows_kernel<8, false, TRAINING><<<grid, 256, 0, st>>>(a, b, cols);
+    return hipGetLastError();
+}
+}  // namespace
+
 hipError_t launch_quantise_rows(const void *Xa, long rows_a, void *codes_a, float *scales_a, const void *Xb, long rows_b, void *codes_b,
-                                float *scales_b, int cols, hipStream_t st)
+                                float *scales_b, int cols, bool training, hipStream_t st)
 {
     const RowsIn a = {(const uint16_t *)Xa, rows_a, (uint8_t *)codes_a, scales_a}, b = {(const uint16_t *)Xb, rows_b, (uint8_t *)codes_b, scales_b};
-    const unsigned grid = (unsigned)(2 * ((rows_a + 31) / 32 + (rows_b + 31) / 32));
-    if (cols <= 1024)      quantise_rows_kernel<4, true><<<grid, 256, 0, st>>>(a, b, cols);
-    else if (cols <= 2048) quantise_rows_kernel<8, true><<<grid, 256, 0, st>>>(a, b, cols);
-    else                   quantise_rows_kernel<8, false><<<grid, 256, 0, st>>>(a, b, cols);
-    return hipGetLastError();
+    return training ? launch_rows<true>(a, b, cols, st) : launch_rows<false>(a, b, cols, st);
 }
 
 struct QkvOut {

@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256) void grad_operands_kernel(const uint16_t *__re
         }
         __syncthreads();
         if (span >= spans) return;                   // nothing below synchronises across waves
-        const float scale = fmaxf(fmaxf(fmaxf(red[0][r], red[1][r]), fmaxf(red[2][r], red[3][r])), 1e-8f) / 448.0f;
+        const float scale = training_scale(fmaxf(fmaxf(red[0][r], red[1][r]), fmaxf(red[2][r], red[3][r])));
         const BlockDivisor divide(scale);
 #pragma unroll
         for (int x = 0; x < 4; ++x) {

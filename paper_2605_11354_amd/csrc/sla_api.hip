@@ -449,7 +449,7 @@ sla_status_t sla_fp8_linear(const void *x, const void *W, const void *bias, int3
     if (workspace_bytes < lp.total) return fail(SLA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, lp.total);
     hipStream_t st = (hipStream_t)stream;
     SLA_HIP(sla::launch_quantise_rows(x, N, at<void>(workspace, lp.off_cx), at<float>(workspace, lp.off_sx), W, d_out,
-                                      at<void>(workspace, lp.off_cw), at<float>(workspace, lp.off_sw), d_in, st));
+                                      at<void>(workspace, lp.off_cw), at<float>(workspace, lp.off_sw), d_in, false, st));
     SLA_HIP(sla::launch_fp8_gemm(at<void>(workspace, lp.off_cx), at<float>(workspace, lp.off_sx), at<void>(workspace, lp.off_cw),
                                  at<float>(workspace, lp.off_sw), bias, N, d_out, d_in, y, st));
     return SLA_OK;
@@ -478,7 +478,7 @@ sla_status_t sla_fp8_linear_qkv(const void *x, const void *W, const void *bias, 
     if (workspace_bytes < lp.total) return fail(SLA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, lp.total);
     hipStream_t st = (hipStream_t)stream;
     SLA_HIP(sla::launch_quantise_rows(x, tokens, at<void>(workspace, lp.off_cx), at<float>(workspace, lp.off_sx), W, d_out,
-                                      at<void>(workspace, lp.off_cw), at<float>(workspace, lp.off_sw), d_in, st));
+                                      at<void>(workspace, lp.off_cw), at<float>(workspace, lp.off_sw), d_in, false, st));
     void *const codes[3] = {Q8, K8, V8};
     float *const scales[3] = {sQ, sK, sV};
     SLA_HIP(sla::launch_fp8_gemm_qkv(at<void>(workspace, lp.off_cx), at<float>(workspace, lp.off_sx), at<void>(workspace, lp.off_cw),
@@ -567,7 +567,7 @@ sla_status_t sla_fp8_linear_save(const void *x, const void *W, const void *bias,
     if ((s = check_buffer("workspace", workspace, workspace_bytes, gp.total)) != SLA_OK) return s;
     hipStream_t st = (hipStream_t)stream;
     float *const sx = at<float>(checkpoint, cp.off_scales), *const sw = at<float>(workspace, gp.off_sw);
-    SLA_HIP(sla::launch_quantise_rows(x, N, checkpoint, sx, W, d_out, workspace, sw, d_in, st));
+    SLA_HIP(sla::launch_quantise_rows(x, N, checkpoint, sx, W, d_out, workspace, sw, d_in, true, st));
     SLA_HIP(sla::launch_fp8_gemm(checkpoint, sx, workspace, sw, bias, N, d_out, d_in, y, st));
     return SLA_OK;
 }

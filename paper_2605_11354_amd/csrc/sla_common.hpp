@@ -136,6 +136,11 @@ struct BlockDivisor {
     }
 };
 
+// The scale of the layer's training form: the product that the formula amax / 448.0 is in PyTorch on the GPU.  It can be a unit in
+// the last place from the quotient, which moves those quotients x / scale that lie half-way between two codes: up to a sixteenth of a row of
+// bf16 values.  It too is never a significand of all ones (tests/test_linear_grad_refusals.py goes through all of them), as BlockDivisor asks.
+__device__ __forceinline__ float training_scale(float amax) { return fmaxf(amax, 1e-8f) * (1.0f / 448.0f); }
+
 // four E4M3 codes of four clamped values (v_cvt_pk_fp8_f32 rounds to nearest even)
 __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d)
 {

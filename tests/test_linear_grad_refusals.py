@@ -1,6 +1,7 @@
 """Refusals of the FP8 layer's training calls: on the host, before any launch."""
 import ctypes as C
 
+import numpy as np
 import pytest
 import torch
 
@@ -71,3 +72,10 @@ def test_tensors_of_another_shape_type_or_place():
         B.sla_fp8_linear_save(x, W, None, y, ck)
     with pytest.raises(ValueError, match="x: "):
         B.sla_fp8_linear_save(x.float(), W, None, y, ck)
+
+
+def test_the_training_scale_is_no_significand_of_ones():
+    """The division step needs that of its divisor: all 128 significands of a bf16 maximum (the scale's exponent plays no part), and 1e-8."""
+    for top in list(np.arange(128, 256, dtype=np.float32)) + [np.float32(1e-8)]:
+        scale = np.float32(top * (np.float32(1) / np.float32(448)))
+        assert scale.view(np.uint32) & 0x7FFFFF != 0x7FFFFF
