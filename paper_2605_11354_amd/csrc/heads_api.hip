@@ -2,6 +2,7 @@
 #include "api_util.hpp"
 #include "sla_kernels.hpp"
 
+#include <algorithm>
 #include <cfloat>
 #include <cmath>
 #include <cstring>
@@ -20,6 +21,7 @@ sla_status_t make_args(const sla_heads_params_t *p, sla::HeadsArgs &a)
     if (p->B < 0 || p->H < 0 || p->N < 0) return fail(SLA_ERR_INVALID_ARG, "B, H, N must be >= 0 (got %d, %d, %d)", p->B, p->H, p->N);
     if (p->D != 64) return fail(SLA_ERR_UNSUPPORTED, "head dim D = %d; only 64 is implemented", p->D);
     if ((long)p->B * p->N > 0x7FFFFF00L) return fail(SLA_ERR_UNSUPPORTED, "B*N = %ld is too large", (long)p->B * p->N);
+    if (p->H > 65535) return fail(SLA_ERR_UNSUPPORTED, "H = %d; at most 65535 are implemented", p->H);
     if ((long)p->B * p->H > 65535) return fail(SLA_ERR_UNSUPPORTED, "B*H = %ld exceeds 65535", (long)p->B * p->H);
     if (p->norm < SLA_NORM_NONE || p->norm > SLA_NORM_LAYER) return fail(SLA_ERR_INVALID_ARG, "unknown norm %d", p->norm);
     if (p->norm_per_head != 0 && p->norm_per_head != 1) return fail(SLA_ERR_INVALID_ARG, "norm_per_head must be 0 or 1");
@@ -35,8 +37,8 @@ sla_status_t make_args(const sla_heads_params_t *p, sla::HeadsArgs &a)
     a.axes = p->axes; a.adjacent = p->pairing == SLA_PAIR_ADJACENT; a.pos_per_item = p->pos_per_item;
     a.bs = p->batch_stride; a.ts = p->token_stride; a.hs = p->head_stride;
     if (a.B && a.H && a.N) {
-        // strides of dimensions of one element do not matter; the others have to keep rows apart: the smaller of the token
-        // and head strides spans a row, the larger one all rows of the smaller, the batch stride all of an item
+        // strides of dimensions of one element do not matter; from the smallest stride on, each of the others has to span all rows
+        // that the smaller ones reach
         const long lim = 1L << 48;
         struct Dim { const char *name; long n; long *s; } dims[3] = {{"head_stride", a.H, &a.hs}, {"token_stride", a.N, &a.ts}, {"batch_stride", a.B, &a.bs}};
         for (Dim &d : dims) {
@@ -44,9 +46,13 @@ sla_status_t make_args(const sla_heads_params_t *p, sla::HeadsArgs &a)
             else if (*d.s < 64 || *d.s % 8 != 0 || *d.s > lim / d.n)
                 return fail(SLA_ERR_INVALID_ARG, "%s = %ld; must be a multiple of 8 and at least 64", d.name, *d.s);
         }
-        const long th = (a.N - 1) * a.ts, hh = (a.H - 1) * a.hs;
-        const bool apart = a.H == 1 || a.N == 1 || (a.hs <= a.ts ? a.ts >= hh + 64 : a.hs >= th + 64);
-        if (!apart || (a.B > 1 && a.bs < th + hh + 64)) return fail(SLA_ERR_INVALID_ARG, "the strides let rows overlap");
+        std::sort(dims, dims + 3, [](const Dim &x, const Dim &y) { return *x.s < *y.s; });
+        long span = 64;
+        for (const Dim &d : dims) {
+            if (d.n == 1) continue;
+            if (*d.s < span) return fail(SLA_ERR_INVALID_ARG, "%s = %ld; the rows of smaller strides reach over %ld elements: rows overlap or interleave", d.name, *d.s, span);
+            span += (d.n - 1) * *d.s;
+        }
     }
     const sla::RowMap out = sla::make_rowmap(p->layout == SLA_LAYOUT_BNHD, p->H, p->N);
     a.obs = out.bs; a.ots = out.ts; a.ohs = out.hs;

@@ -456,9 +456,9 @@ __global__ __launch_bounds__(256, 3) void heads_grad_kernel(HeadsArgs a, HeadsGr
 __global__ __launch_bounds__(1024) void heads_grad_reduce_kernel(const float *__restrict__ part, int slots, int heads, HeadsGrads d)
 {
     __shared__ float sums[64][16];
-    const int c = threadIdx.x & 15, s = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
-    const int tensor = blockIdx.y / heads, head = blockIdx.y - tensor * heads;
-    const float *const p = part + (size_t)blockIdx.y * slots * 128 + col;
+    const int c = threadIdx.x & 15, s = threadIdx.x >> 4, col = (blockIdx.x & 7) * 16 + c;
+    const int pair = blockIdx.x >> 3, tensor = pair / heads, head = pair - tensor * heads;
+    const float *const p = part + (size_t)pair * slots * 128 + col;
     float v = 0.f;
 #pragma unroll 4
     for (int k = s; k < slots; k += 64) v += p[(size_t)k * 128];
@@ -540,7 +540,7 @@ template <int ROT> hipError_t launch_heads_grad_rot(HeadsArgs a, HeadsGrads d, h
     }
     if (!d.part && !d.dw[0] && !d.dw[1] && !d.db[0] && !d.db[1]) return hipSuccess;
     const int heads = a.per_head ? a.H : 1;
-    heads_grad_reduce_kernel<<<dim3(8, 2 * heads), 1024, 0, st>>>(d.part, d.slots, heads, d);
+    heads_grad_reduce_kernel<<<16u * heads, 1024, 0, st>>>(d.part, d.slots, heads, d);
     return hipGetLastError();
 }
 }  // namespace

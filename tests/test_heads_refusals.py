@@ -44,7 +44,8 @@ def grad(lib, p, dV=PTR, dv=PTR, dqw=PTR, ws=PTR, size=1 << 20, dq=PTR):
     (dict(token_stride=-576), B.SLA_ERR_INVALID_ARG), (dict(token_stride=0), B.SLA_ERR_INVALID_ARG),
     (dict(token_stride=1 << 60), B.SLA_ERR_INVALID_ARG),
     (dict(head_stride=60), B.SLA_ERR_INVALID_ARG), (dict(head_stride=68), B.SLA_ERR_INVALID_ARG),
-    (dict(batch_stride=576), B.SLA_ERR_INVALID_ARG), (dict(batch_stride=0), B.SLA_ERR_INVALID_ARG),
+    (dict(H=70000, B=0), B.SLA_ERR_UNSUPPORTED), (dict(H=1 << 30, N=0, B=0, norm_per_head=1), B.SLA_ERR_UNSUPPORTED),
+    (dict(batch_stride=576), B.SLA_ERR_INVALID_ARG), (dict(batch_stride=640), B.SLA_ERR_INVALID_ARG), (dict(batch_stride=128), B.SLA_ERR_INVALID_ARG), (dict(batch_stride=0), B.SLA_ERR_INVALID_ARG),
 ])
 def test_parameters(lib, kw, status):
     p = params(**kw)
@@ -83,9 +84,10 @@ def test_nothing_to_do(lib, kw):
     assert B.sla_qk_norm_rope_grad_workspace_bytes(p) == 0
 
 
-def test_strides_of_single_elements_do_not_matter(lib):
+def test_orders_of_dimensions_and_strides_of_single_elements_do_not_matter(lib):
     n = C.c_size_t()
-    for kw in (dict(B=1, batch_stride=-7), dict(N=1, token_stride=0), dict(H=1, head_stride=3)):
+    for kw in (dict(token_stride=1152, batch_stride=576), dict(token_stride=64, head_stride=320, batch_stride=960),       # other orders of the dimensions
+               dict(B=1, batch_stride=-7), dict(N=1, token_stride=0), dict(H=1, head_stride=3)):
         assert lib.sla_qk_norm_rope_grad_workspace_bytes(C.byref(params(**kw)), C.byref(n)) == B.SLA_OK
 
 
