@@ -359,6 +359,8 @@ hipError_t launch_dequantise_mxfp4(const void *codes, const void *scales, long r
     return hipGetLastError();
 }
 
+// One launch while quantising x in every workgroup costs less than a launch of its own: 32 tokens through 4096 x 4096 11.6 us (13.1 with two launches), 1024 x 1024 4.7 (6.9);
+// 48 tokens, in tiles of 64, 17.0 (13.0) and 6.3 (6.9).
 bool mxfp4_few(int M) { return M <= 32; }
 
 namespace {
@@ -389,13 +391,20 @@ hipError_t launch_mxfp4_few(const void *X, const void *W, const void *Ws, const 
     return launch_few<2>(X, W, Ws, bias, M, O, K, Y, st);
 }
 
+// W by steps costs its quantiser launch (17/32 O K bytes read and written): where both products take as long as that, with M = O
+// (4096 tokens x 4096 -> 4096: 53.2 us as it lies, 51.6 turned; 4096 x 1024 -> 4096: 21.3 both), it is not worth the workspace; with M = 2 O it is
+// (8192 x 4096 -> 4096: 100 and 95; 8192 x 1024 -> 4096: 36.2 and 34.6).
 bool mxfp4_turns_weights(int M, int O) { return M >= 2L * O; }
 
+// Tiles.  64 x 128 while each has a CU of its own (256 of them, 2048 x 1024 -> 1024: 6.1 us, 6.7 with 128 x 128; 352, 700 x 1024 -> 4096: 7.5 and
+// 7.0, from 4096 channels 23.3 and 17.0).  A 256 x 256 tile reads half as much from LDS and L2 for a product as four of 128 x 128, but has a CU to
+// itself, with nothing under its start and end: from 192 on (172, 10992 x 1024 -> 1024: 15.2 us and 12.9; 192, 3000 x 1024 -> 4096: 16.0 and 14.0,
+// x 4096: 34.8 and 41.0; 2752, 43968 x 1024 -> 4096: 155 and 158; 688, 43968 x 4096 -> 1024: 102 and 108).
 hipError_t launch_mxfp4_gemm(const void *A, const void *As, const void *W, const void *Ws, bool by_steps, const void *bias, int M, int O, int K, void *Y, hipStream_t st)
 {
-    const long wide = (long)((M + 255) / 256) * ((O + 255) / 256), n_ot = (O + 127) / 128;
-    if (wide >= 160) return launch_gemm<4, 4>(A, As, W, Ws, by_steps, bias, M, O, K, Y, st);
-    if ((M + 127) / 128 * n_ot >= 400) return launch_gemm<2, 2>(A, As, W, Ws, by_steps, bias, M, O, K, Y, st);
+    const long wide = (long)((M + 255) / 256) * ((O + 255) / 256), narrow = (long)((M + 63) / 64) * ((O + 127) / 128);
+    if (wide >= 192) return launch_gemm<4, 4>(A, As, W, Ws, by_steps, bias, M, O, K, Y, st);
+    if (narrow > 256) return launch_gemm<2, 2>(A, As, W, Ws, by_steps, bias, M, O, K, Y, st);
     return launch_gemm<1, 2>(A, As, W, Ws, by_steps, bias, M, O, K, Y, st);
 }
 
