@@ -22,6 +22,13 @@ __device__ __forceinline__ uint32_t top_bits(uint4 u)
     const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(mag(u.x), mag(u.y)), __builtin_elementwise_max(mag(u.z), mag(u.w)));
     return m[0] > m[1] ? m[0] : m[1];
 }
+// of a block, eight elements in each of four neighbouring lanes
+__device__ __forceinline__ uint32_t block_top(uint4 u)
+{
+    uint32_t top = top_bits(u);
+    top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0xB1, 0xf, 0xf, true));
+    return max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0x4E, 0xf, 0xf, true));
+}
 // scale byte of a block with that largest magnitude
 __device__ __forceinline__ uint32_t scale_byte(uint32_t top) { return top >= 0x7F80u ? 255u : (top >> 7) < 2 ? 0u : (top >> 7) - 2; }
 
@@ -66,10 +73,7 @@ __global__ __launch_bounds__(256) void quantise_mxfp4_kernel(const uint4 *__rest
         }
     if (at >= pieces) return;
     const uint4 u = X[at];
-    uint32_t top = top_bits(u);
-    top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0xB1, 0xf, 0xf, true));
-    top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0x4E, 0xf, 0xf, true));
-    const uint32_t s = scale_byte(top), code = s == 255 ? 0u : codes8(u, scale_value(s));
+    const uint32_t s = scale_byte(block_top(u)), code = s == 255 ? 0u : codes8(u, scale_value(s));
     if constexpr (BY_STEPS) {
         const unsigned row = (unsigned)at / (16u * steps), q = (unsigned)at - row * 16u * steps, st = q >> 4;
         codes[((size_t)(row >> 4) * steps + st) * 256 + (row & 15) * 16 + (q & 15)] = code;
@@ -277,42 +281,65 @@ __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void mxfp4_gemm_kernel(const 
     }, lane, M - tok0, O - ch0, Y + (size_t)tok0 * O + ch0, (size_t)O);
 }
 
-// Few tokens (at most 16 T): one launch, bound by the weights' bytes and by latency.  A wave takes 16 channels and a part of K
-// in steps of 128: lane l holds the 32 elements 32 (l / 16) .. of row l % 16, one whole block, both of W (as it lies) and of
-// x, which it quantises by itself; no LDS and no exchange between lanes before the waves' sums are added, in order.
-// `parts` waves (a power of two) share 16 channels, 8 / parts groups of channels share a workgroup.
-template <int T>
+// Few tokens (at most 4 Q): one launch, bound by the weights' bytes and by latency.  A wave takes 16 channels and a part of K
+// in steps of 128: of W lane l holds the 32 elements 32 (l / 16) .. of row l % 16, one whole block, as it lies.  x is quantised on the way:
+// sixteen lanes read the 256 bytes of a token's step, four to a block, and the codes and scales go through the wave's own LDS to the lanes
+// that multiply them.  The next step's bytes are asked for before this one's are used (two or four steps ahead take registers from other
+// workgroups: 4 tokens, 1152 -> 8208 3.8 us and 4.7).  Without a condition on the number of tokens inside, the four tokens' forty instructions each
+// go into one another: 16 tokens through 4096 x 4096 6.8 us and 5.8.  One token: 4.6 us for 8.9 MB of weights, four steps of latency and a launch.
+// `parts` waves (a power of two) share 16 channels, 8 / parts groups of channels share a workgroup; their sums are added in order.
+template <int Q>
 __global__ __launch_bounds__(512) void mxfp4_few_kernel(const uint16_t *__restrict__ X, const uint8_t *__restrict__ W, const uint8_t *__restrict__ Ws,
                                                         const uint16_t *__restrict__ bias, int M, int O, int K, int parts, uint16_t *__restrict__ Y)
 {
+    constexpr int T = (Q + 3) / 4;                   // sixteens of tokens
     __shared__ float sums[8][T][16][17];             // [wave][16 tokens][token][channel]
+    __shared__ __attribute__((aligned(16))) uint32_t x_codes[8][T][256];         // [wave][16 tokens][token][block][dword]
+    __shared__ uint8_t x_scales[8][T][64];                                       // [wave][16 tokens][token][block]
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, r16 = lane & 15, c = lane >> 4;
     const int part = wave & (parts - 1), group = wave / parts, o0 = ((int)blockIdx.x * (8 / parts) + group) * 16;
-    const int steps = K / 128, per = (steps + parts - 1) / parts, s0 = part * per, s1 = min(steps, s0 + per);
+    const int steps = K / 128, mine = (steps - part + parts - 1) / parts;        // steps part, part + parts, ...: at least one
     const int o = min(o0 + r16, O - 1);              // rows past the end repeat the last one
     f32x4 acc[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     const uint8_t *const w = W + (size_t)o * (K / 2) + c * 16, *const ws = Ws + (size_t)o * (K / 32) + c;
-    const uint16_t *x[T];
+    const uint16_t *x[Q];                            // instruction j reads tokens 4 j + l / 16; those past the end repeat the last one
 #pragma unroll
-    for (int t = 0; t < T; ++t) x[t] = X + (size_t)min(16 * t + r16, M - 1) * K + c * 32;
-    for (int s = s0; s < s1; ++s) {
-        const uint4 u = *(const uint4 *)(w + s * 64);
-        const int sw = ws[s * 4];
-        const i32x8 wf = {(int)u.x, (int)u.y, (int)u.z, (int)u.w, 0, 0, 0, 0};
+    for (int j = 0; j < Q; ++j) x[j] = X + (size_t)min(4 * j + c, M - 1) * K + 8 * r16;
+    uint4 wn, xn[Q];
+    uint32_t sn;
+    auto load = [&](int k) {                         // the wave's step k
+        const int s = part + parts * k;
+        wn = *(const uint4 *)(w + s * 64);
+        sn = ws[s * 4];
+#pragma unroll
+        for (int j = 0; j < Q; ++j) xn[j] = *(const uint4 *)(x[j] + s * 128);
+    };
+    load(0);
+    if (Q < 4) {                                     // tokens that are not there: zeros
+        *(uint4 *)(x_codes[wave][0] + 4 * lane) = make_uint4(0, 0, 0, 0);
+        x_scales[wave][0][lane] = 0;
+        wave_lds_sync();
+    }
+    for (int k = 0; k < mine; ++k) {
+        const i32x8 wf = {(int)wn.x, (int)wn.y, (int)wn.z, (int)wn.w, 0, 0, 0, 0};
+        const int sw = (int)sn;
+#pragma unroll
+        for (int j = 0; j < Q; ++j) {
+            const uint32_t sx = scale_byte(block_top(xn[j]));
+            x_codes[wave][j / 4][64 * (j % 4) + lane] = codes8(xn[j], scale_value(sx)) & (sx == 255 ? 0u : ~0u);
+            x_scales[wave][j / 4][16 * (j % 4) + (lane >> 2)] = (uint8_t)sx;
+        }
+        if (k + 1 < mine) load(k + 1);
+        wave_lds_sync();
 #pragma unroll
         for (int t = 0; t < T; ++t) {
-            uint4 v[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] = *(const uint4 *)(x[t] + s * 128 + 8 * q);
-            const uint32_t sx = scale_byte(max(max(top_bits(v[0]), top_bits(v[1])), max(top_bits(v[2]), top_bits(v[3]))));
-            const float scale = scale_value(sx);
-            i32x8 xf = {};
-#pragma unroll
-            for (int q = 0; q < 4; ++q) xf[q] = sx == 255 ? 0 : (int)codes8(v[q], scale);
-            acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf, xf, acc[t], kFp4, kFp4, 0, sw, 0, (int)sx);
+            const uint4 u = *(const uint4 *)(x_codes[wave][t] + 16 * r16 + 4 * c);
+            const i32x8 xf = {(int)u.x, (int)u.y, (int)u.z, (int)u.w, 0, 0, 0, 0};
+            acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf, xf, acc[t], kFp4, kFp4, 0, sw, 0, (int)x_scales[wave][t][4 * r16 + c]);
         }
+        wave_lds_sync();
     }
     // register r of acc[t]: channel 4 c + r, token 16 t + r16
 #pragma unroll
@@ -359,17 +386,17 @@ hipError_t launch_dequantise_mxfp4(const void *codes, const void *scales, long r
     return hipGetLastError();
 }
 
-// One launch while quantising x in every workgroup costs less than a launch of its own: 32 tokens through 4096 x 4096 11.6 us (13.1 with two launches), 1024 x 1024 4.7 (6.9);
-// 48 tokens, in tiles of 64, 17.0 (13.0) and 6.3 (6.9).
+// One launch while quantising x in every workgroup costs less than a launch of its own: 32 tokens through 4096 x 4096 8.9 us (12.7 with two launches),
+// 1024 x 1024 4.1 (6.9), 1152 -> 8208 7.3 (7.1); every four tokens more cost 0.8, 0.2 and 0.7 us here and nothing there.
 bool mxfp4_few(int M) { return M <= 32; }
 
 namespace {
-template <int T> hipError_t launch_few(const void *X, const void *W, const void *Ws, const void *bias, int M, int O, int K, void *Y, hipStream_t st)
+template <int Q> hipError_t launch_few(const void *X, const void *W, const void *Ws, const void *bias, int M, int O, int K, void *Y, hipStream_t st)
 {
     int parts = 1;                                   // waves that share a channel group's K, each with a step at least
     while (parts < 8 && 2 * parts <= K / 128) parts *= 2;
     const int channels = 16 * (8 / parts);
-    mxfp4_few_kernel<T><<<(unsigned)((O + channels - 1) / channels), 512, 0, st>>>((const uint16_t *)X, (const uint8_t *)W, (const uint8_t *)Ws,
+    mxfp4_few_kernel<Q><<<(unsigned)((O + channels - 1) / channels), 512, 0, st>>>((const uint16_t *)X, (const uint8_t *)W, (const uint8_t *)Ws,
                                                                                   (const uint16_t *)bias, M, O, K, parts, (uint16_t *)Y);
     return hipGetLastError();
 }
@@ -387,8 +414,10 @@ hipError_t launch_gemm(const void *A, const void *As, const void *W, const void 
 
 hipError_t launch_mxfp4_few(const void *X, const void *W, const void *Ws, const void *bias, int M, int O, int K, void *Y, hipStream_t st)
 {
-    if (M <= 16) return launch_few<1>(X, W, Ws, bias, M, O, K, Y, st);
-    return launch_few<2>(X, W, Ws, bias, M, O, K, Y, st);
+    if (M <= 4) return launch_few<1>(X, W, Ws, bias, M, O, K, Y, st);
+    if (M <= 8) return launch_few<2>(X, W, Ws, bias, M, O, K, Y, st);
+    if (M <= 16) return launch_few<4>(X, W, Ws, bias, M, O, K, Y, st);
+    return launch_few<8>(X, W, Ws, bias, M, O, K, Y, st);
 }
 
 // W by steps costs its quantiser launch (17/32 O K bytes read and written): where both products take as long as that, with M = O
