@@ -411,27 +411,27 @@ int even_splits(int steps, long most)
 }
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
-// Tiles and splits.  256 x 256 tiles reach 1.2 PFLOP/s, 128 x 128 tiles 0.85, where either fills the chip; what speaks for the
-// small ones is that a sum split less often leaves fewer partials (fp32, written and read again).
-//   dx  wide from 160 tiles on: 10992 x 1024 (172 wide tiles, 688 narrow ones) takes the same either way; else narrow, and split where
-//       there are fewer than 256 (few tokens), into parts of at least eight steps
-//   dW  wide where eight splits are enough for 256 workgroups (1024 x 1024 over 10992 tokens: 64 narrow tiles in 8 splits 32 us and 6 for
-//       the partials, 16 wide ones in 16 splits 34 and 11)
+// Tiles and splits.  256 x 256 tiles reach 1.2 PFLOP/s, 128 x 128 tiles 0.85, where either fills the chip; what speaks for the small ones is that
+// half a round of them is less, and that a sum split less often leaves fewer partials (fp32, written and read again).  Both products
+// take the same, so that one launch has them: where one ends the other fills its CUs (10992 tokens, 1024 -> 1024: 78 us in launches of 256 for
+// dx and of 128 for dW, 70 in one of 128).  256 from 128 such tiles of dx and 100 steps of both products for each CU on:
+//     us, 128 and 256:   43968 tokens, 1024 -> 1024 (172 steps) 231, 225;  10992, 1024 -> 4096 (172) 215, 196;  2048, 4096 -> 4096 (128) 206, 191;
+//     21984, 1024 -> 1024 (86) 119, 133;  5496, 4096 -> 1024 (86) 153, 142;  43968, 384 -> 1152 (73) 102, 134;  4096, 1024 -> 4096 (64) 90, 139
+//   dx  128 wide: split where there are fewer than 256 tiles (few tokens), into parts of at least eight steps
+//   dW  split into workgroups for the whole chip: 256, or 512 of the small ones, into parts of at least eight steps
 struct Plan {
-    bool wide_x, wide_w;
+    bool wide;
     int splits_x, splits_w;
     size_t off_bx, off_part_x, off_part_w, off_part_db, total;                   // the operand of dx comes first
 };
 Plan make_plan(int N, int d_in, int d_out)
 {
     Plan p;
-    p.wide_x = tiles_of(N, d_in, 256) >= 160;
-    const long tx = tiles_of(N, d_in, 128);
-    p.splits_x = p.wide_x || !N ? 1 : even_splits((d_out + kStepK - 1) / kStepK, tx >= 256 ? 1 : std::min(256 / tx, (long)(d_out / (8 * kStepK))));
-    const int steps = (N + kStepK - 1) / kStepK;
-    const long tw = tiles_of(d_out, d_in, 256);
-    p.wide_w = tw >= 32 && tw * (steps / 8) >= 256;
-    p.splits_w = even_splits(steps, std::min(p.wide_w ? 256 / tw : 512 / tiles_of(d_out, d_in, 128), (long)steps / 8));
+    const long x256 = tiles_of(N, d_in, 256), w256 = tiles_of(d_out, d_in, 256), x128 = tiles_of(N, d_in, 128), w128 = tiles_of(d_out, d_in, 128);
+    const int x_steps = (d_out + kStepK - 1) / kStepK, w_steps = (N + kStepK - 1) / kStepK;
+    p.wide = x256 >= 128 && x256 * x_steps + w256 * w_steps >= 100 * 256;
+    p.splits_x = p.wide || !N ? 1 : even_splits(x_steps, x128 >= 256 ? 1 : std::min(256 / x128, (long)x_steps / 8));
+    p.splits_w = even_splits(w_steps, std::min(p.wide ? 256 / w256 : 512 / w128, (long)w_steps / 8));
     p.off_bx = (size_t)((d_out + 31) / 32) * 64 * d_in;
     p.off_part_x = p.off_bx + (size_t)((N + 31) / 32) * 64 * d_in;
     p.off_part_w = p.off_part_x + (p.splits_x > 1 ? up256((size_t)p.splits_x * N * d_in * 4) : 0);
@@ -482,22 +482,18 @@ hipError_t launch_linear_grad(const void *dy, const void *x8, const float *sx, c
         if (dx) {
             x.A = (const uint16_t *)dy; x.B = bw; x.lda = d_out; x.M = N; x.cols = d_in; x.K = d_out; x.C = (uint16_t *)dx;
             x.part = p.splits_x > 1 ? (float *)(ws + p.off_part_x) : nullptr;
-            if (!set_product(x, p.wide_x, p.splits_x)) return hipErrorInvalidValue;
+            if (!set_product(x, p.wide, p.splits_x)) return hipErrorInvalidValue;
             if (x.part) add(0, x.part, dx, (long)N * d_in, p.splits_x);
         }
         if (dW) {
             w.A = (const uint16_t *)dy; w.B = bx; w.lda = d_out; w.M = d_out; w.cols = d_in; w.K = N; w.C = (uint16_t *)dW; w.db = (uint16_t *)db;
             w.part = p.splits_w > 1 ? (float *)(ws + p.off_part_w) : nullptr;
             w.part_db = (float *)(ws + p.off_part_db);
-            if (!set_product(w, p.wide_w, p.splits_w)) return hipErrorInvalidValue;
+            if (!set_product(w, p.wide, p.splits_w)) return hipErrorInvalidValue;
             if (w.part) add(1, w.part, dW, (long)d_out * d_in, p.splits_w);
             if (w.part && db) add(2, w.part_db, db, d_out, p.splits_w);
         }
-        if (dx && dW && p.wide_x != p.wide_w) {
-            const GradProduct none = {};
-            if ((e = launch_products(p.wide_w, w, none, st)) != hipSuccess) return e;
-            e = launch_products(p.wide_x, none, x, st);
-        } else e = launch_products(dW ? p.wide_w : p.wide_x, w, x, st);
+        e = launch_products(p.wide, w, x, st);
         if (e != hipSuccess) return e;
     } else {                                         // no tokens: sums of nothing
         if (dW) add(1, nullptr, dW, (long)d_out * d_in, 0);

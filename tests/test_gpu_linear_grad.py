@@ -166,3 +166,27 @@ def test_codes_are_pytorch_s():
     scale = x.float().abs().amax(1, keepdim=True).clamp(min=1e-8) / 448.0
     want = (x.float() / scale).clamp(-448.0, 448.0).to(torch.float8_e4m3fn).float() * scale
     assert torch.equal(xq, want.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("N,d_in,d_out", [(8213, 1152, 3208), (33001, 256, 4104)])
+def test_large_tiles(N, d_in, d_out):
+    """Sizes of the largest tiles, with ends inside a tile and inside a step on all three axes; fp64 products on the device."""
+    x, W, b, dy = layer(N, d_in, d_out, 3)
+    X, Wd, bd, dyd = map(G.dev_bf16, (x, W, b, dy))
+    ck, ws, y, dx, dW, db = buffers(N, d_in, d_out)
+    B.sla_fp8_linear_save(X, Wd, bd, y, ck[:-256], ws[:-256])
+    B.sla_fp8_linear_grad(dyd, ck[:-256], Wd, dx, dW, db, ws[:-256])
+    (xc, xs), (wc, wsc) = po.e4m3_rows(x), po.e4m3_rows(W)
+    xq, wq = (torch.from_numpy(c * s[:, None]).cuda() for c, s in ((xc, xs), (wc, wsc)))
+    g = dyd.double()
+    for got, a, q, K, what in ((dx, g, wq, d_out, "dx"), (dW, g.T, xq, N, "dW")):
+        ref, mag = a @ q, a.abs() @ q.abs()
+        d = (got.double() - ref).abs()
+        assert bool((d <= 2.0 ** -8 * ref.abs() + (2.0 ** -8 + (K + 20) * 2.0 ** -24) * mag).all()), (what, float(d.max()))
+        assert float(torch.linalg.norm(got.double() - ref)) <= 3.2e-3 * float(torch.linalg.norm(ref)), what
+    ref, mag = g.sum(0), g.abs().sum(0)
+    assert bool(((db.double() - ref).abs() <= 2.0 ** -8 * ref.abs() + (N + 20) * 2.0 ** -24 * mag).all())
+    ref = xq @ wq.T + bd.double()
+    mag = xq.abs() @ wq.abs().T + bd.double().abs()
+    assert bool(((y.double() - ref).abs() <= 2.0 ** -8 * ref.abs() + (d_in + 4) * 2.0 ** -24 * mag).all())
+    assert bool((ck[-256:] == 0x5A).all()) and bool((ws[-256:] == 0x5A).all())
