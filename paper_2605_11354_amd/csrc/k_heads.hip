@@ -22,8 +22,8 @@
 namespace sla {
 
 namespace {
-// floats per token of the table: 32 cosines, 32 sines, 32 negated sines (BOTH, where there is room for them), one 16-byte step of padding
-template <bool BOTH> constexpr int kCsPitch = BOTH ? 100 : 68;
+// floats per token of the table: 32 cosines, 32 sines, 32 negated sines, one 16-byte step of padding
+constexpr int kCsPitch = 100;
 
 // The group of eight channels that lane c of a row's eight holds: 0 1 2 3 7 6 5 4, so that the partner of a pair (i, i + 32) is the
 // lane mirrored within eight, and that of (i, i + 16) within a half of 32 the lane two on or back: one DPP operand either way.
@@ -63,12 +63,12 @@ __device__ __forceinline__ uint4 packed8(const float (&x)[8])
 
 // n rotated by the angles of its token (back = 0) or back (1); o = the lane's group of eight channels, cs = the token's
 // row of the table.  ROT: 1 = channels (i, i + 32) are a pair, 2 = (i, i + 16) within each half of 32, 3 = (2 i, 2 i + 1)
-template <int ROT, bool BOTH = true> __device__ __forceinline__ void rotate(float (&n)[8], const float *cs, int o, int back)
+template <int ROT> __device__ __forceinline__ void rotate(float (&n)[8], const float *cs, int o, int back)
 {
     if constexpr (ROT == 1 || ROT == 2) {
         const int at = ROT == 1 ? 8 * (o & 3) : 16 * (o >> 2) + 8 * (o & 1);
         const bool adds = ((o & (ROT == 1 ? 4 : 2)) != 0) != (back != 0);       // the second of a pair adds, the first subtracts
-        const int sines = adds || !BOTH ? 32 : 64;
+        const int sines = adds ? 32 : 64;
         float c[8], s[8];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -78,10 +78,10 @@ template <int ROT, bool BOTH = true> __device__ __forceinline__ void rotate(floa
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float p = partner<ROT>(n[e]);
-            n[e] = fmaf(p, BOTH || adds ? s[e] : -s[e], n[e] * c[e]);
+            n[e] = fmaf(p, s[e], n[e] * c[e]);
         }
     } else if constexpr (ROT == 3) {
-        const float4 c4 = *(const float4 *)(cs + 4 * o), s4 = *(const float4 *)(cs + (BOTH && back ? 64 : 32) + 4 * o);
+        const float4 c4 = *(const float4 *)(cs + 4 * o), s4 = *(const float4 *)(cs + (back ? 64 : 32) + 4 * o);
         const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -110,12 +110,22 @@ __device__ __forceinline__ float normalise(float (&x)[8], int norm, float eps)
     return r;
 }
 
-// cos and sin of `quarters` quarter turns, reduced in 64 bits: a position of 2^31 still leaves 2^-22 of a turn.  Taylor series on half a
-// quarter to either side: the first terms left out are below 3e-8.
-__device__ __forceinline__ float2 cos_sin(double quarters)
+// cos and sin of position * turn quarter turns (hi, lo: turn as the sum of two fp32).  Up to 2^20 the whole quarters, rounded from an fp32 product, are off
+// by at most 2^-5, and what is left of position * hi is exact before its one rounding; beyond, 64 bits: a position of 2^31 still leaves
+// 2^-22 of a turn.  Taylor series on 0.54 of a quarter to either side: the first terms left out are below 5e-8.
+__device__ __forceinline__ float2 cos_sin(int position, float hi, float lo, double turn)
 {
-    const double whole = rint(quarters);
-    const float t = (float)(quarters - whole) * 1.57079632679f, z = t * t;
+    float whole, left;
+    if (position > -(1 << 20) && position < 1 << 20) {
+        const float p = (float)position;
+        whole = rintf(p * hi);
+        left = fmaf(p, lo, fmaf(p, hi, -whole));
+    } else {
+        const double quarters = (double)position * turn, w = rint(quarters);
+        left = (float)(quarters - w);
+        whole = (float)(w - 4.0 * rint(0.25 * w));    // all that counts of it
+    }
+    const float t = left * 1.57079632679f, z = t * t;
     const float s = t * fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.0f / 362880.0f, -1.0f / 5040.0f), 1.0f / 120.0f), -1.0f / 6.0f), 1.0f);
     const float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.0f / 40320.0f, -1.0f / 720.0f), 1.0f / 24.0f), -0.5f), 1.0f);
     const int q = (int)whole;
@@ -134,23 +144,24 @@ __device__ __forceinline__ void lay_out_tokens(const HeadsArgs &a, int b, long f
         const int item = SEQ ? b : (int)((unsigned)f / (unsigned)a.N), t = SEQ ? (int)f : (int)f - item * a.N;
         in_off[tid] = item * a.bs + t * a.ts;
         out_off[tid] = item * a.obs + t * a.ots;
-        pos_row[tid] = a.pos_per_item ? item * a.N + t : t;
+        if constexpr (!SEQ) pos_row[tid] = a.pos_per_item ? item * a.N + t : t;
     }
     __syncthreads();
 }
 // Their angles
-template <bool BOTH = true>
-__device__ __forceinline__ void make_table(const HeadsArgs &a, int valid, const int *pos_row, float *table)
+template <class Row>
+__device__ __forceinline__ void make_table(const HeadsArgs &a, int valid, Row pos_row, float *table)
 {
     const int tid = threadIdx.x, j = tid & 31, per = 32 / a.axes, axis = j / per;
     const double turn = a.turn[j];
+    const float hi = (float)turn, lo = (float)(turn - hi);
     const int rows = (valid + 7) & ~7;               // whole groups of eight: the rows behind the last one repeat it, here too
     for (int r = tid >> 5; r < rows; r += 8) {
-        const float2 cs = cos_sin((double)a.pos[(size_t)pos_row[r] * a.axes + axis] * turn);
-        float *const row = table + r * kCsPitch<BOTH>;
+        const float2 cs = cos_sin(a.pos[(size_t)pos_row(r) * a.axes + axis], hi, lo, turn);
+        float *const row = table + r * kCsPitch;
         row[j] = cs.x;
         row[32 + j] = cs.y;
-        if constexpr (BOTH) row[64 + j] = -cs.y;
+        row[64 + j] = -cs.y;
     }
     lds_barrier();
 }
@@ -187,7 +198,7 @@ __global__ __launch_bounds__(256, 4) void heads_kernel(HeadsArgs a)
     constexpr int kOct = TOK / 8, kItems = ROWS / kOct;
     __shared__ long in_off[TOK], out_off[TOK];
     __shared__ int pos_row[TOK];
-    __shared__ __attribute__((aligned(16))) float table[ROT ? TOK * kCsPitch<true> : 4];
+    __shared__ __attribute__((aligned(16))) float table[ROT ? TOK * kCsPitch : 4];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, o = channel_group(lane & 7), r0 = lane >> 3;
     const unsigned blk = blockIdx.x / (unsigned)a.splits, part = blockIdx.x - blk * (unsigned)a.splits;
     const long first = (long)blk * TOK;
@@ -204,7 +215,7 @@ __global__ __launch_bounds__(256, 4) void heads_kernel(HeadsArgs a)
             }
     };
     load(i0 + wave * kItems);
-    if constexpr (ROT != 0) make_table(a, valid, pos_row, table);
+    if constexpr (ROT != 0) make_table(a, valid, [&](int r) { return (long)pos_row[r]; }, table);
     float w[8], bias[8];
     int have = -1;                                   // tensor whose weights these are
     for (int unit = i0 + wave * kItems; unit < i1; unit += 4 * kItems) {
@@ -231,7 +242,7 @@ __global__ __launch_bounds__(256, 4) void heads_kernel(HeadsArgs a)
                 (void)normalise(x, a.norm, a.eps);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = fmaf(x[e], w[e], bias[e]);
-                if constexpr (ROT != 0) rotate<ROT>(x, table + r * kCsPitch<true>, o, 0);
+                if constexpr (ROT != 0) rotate<ROT>(x, table + r * kCsPitch, o, 0);
                 rows[k] = packed8(x);
             }
             if (r < valid) *(uint4 *)((uint16_t *)pick(a.y, it.tensor) + out_off[r] + it.head * a.ohs + 8 * o) = rows[k];
@@ -247,16 +258,15 @@ __global__ __launch_bounds__(256, 3) void heads_e4m3_kernel(HeadsArgs a)
 {
     constexpr int kTok = 64 * SUB, kAtOnce = 4 / SUB;
     __shared__ long in_off[kTok], out_off[kTok];
-    __shared__ int pos_row[kTok];
     __shared__ float red[2][4];
-    __shared__ __attribute__((aligned(16))) float table[ROT ? kTok * kCsPitch<SUB == 1> : 4];
+    __shared__ __attribute__((aligned(16))) float table[ROT ? kTok * kCsPitch : 4];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, o = channel_group(lane & 7), r0 = lane >> 3;
     const unsigned blk = blockIdx.x / (unsigned)a.splits, part = blockIdx.x - blk * (unsigned)a.splits;
     const unsigned per = (unsigned)(a.N + kTok - 1) / kTok;
     const int b = (int)(blk / per);
     const long first = (long)(blk - (unsigned)b * per) * kTok;
     const int valid = (int)min((long)kTok, a.N - first);
-    lay_out_tokens<kTok, true>(a, b, first, valid, in_off, out_off, pos_row);
+    lay_out_tokens<kTok, true>(a, b, first, valid, in_off, out_off, nullptr);
 
     const int sub = SUB == 2 ? wave & 1 : 0, row0 = 64 * sub + r0, mine = min(64, valid - 64 * sub);      // this wave's tokens
     const int i0 = (int)part * a.chunk, i1 = min(i0 + a.chunk, a.tensors * a.H);
@@ -271,7 +281,7 @@ __global__ __launch_bounds__(256, 3) void heads_e4m3_kernel(HeadsArgs a)
             if (8 * k < mine) rows[k] = *(const uint4 *)(x + in_off[row0 + 8 * k]);
     };
     load(at0);
-    if constexpr (ROT != 0) make_table<SUB == 1>(a, valid, pos_row, table);
+    if constexpr (ROT != 0) make_table(a, valid, [&](int r) { return (a.pos_per_item ? (long)b * a.N : 0) + first + min(r, valid - 1); }, table);
     for (int s = 0; s < steps; ++s) {
         const int item = at0 + s * kAtOnce;
         const bool active = item < i1 && mine > 0;
@@ -291,7 +301,7 @@ __global__ __launch_bounds__(256, 3) void heads_e4m3_kernel(HeadsArgs a)
                     (void)normalise(y[k], a.norm, a.eps);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) y[k][e] = fmaf(y[k][e], w[e], bias[e]);
-                    if constexpr (ROT != 0) rotate<ROT, SUB == 1>(y[k], table + (row0 + 8 * k) * kCsPitch<SUB == 1>, o, 0);
+                    if constexpr (ROT != 0) rotate<ROT>(y[k], table + (row0 + 8 * k) * kCsPitch, o, 0);
                 }
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) amax = fmaxf(amax, fmaxf(fabsf(y[k][e]), fabsf(y[k][e + 1])));
@@ -342,7 +352,7 @@ __global__ __launch_bounds__(256, 3) void heads_grad_kernel(HeadsArgs a, HeadsGr
     constexpr int kOct = TOK / 8, kItems = 64 / TOK;
     __shared__ long in_off[TOK], out_off[TOK];
     __shared__ int pos_row[TOK];
-    __shared__ __attribute__((aligned(16))) float table[ROT ? TOK * kCsPitch<true> : 4];
+    __shared__ __attribute__((aligned(16))) float table[ROT ? TOK * kCsPitch : 4];
     __shared__ __attribute__((aligned(16))) float sums[4][2][128];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, o = channel_group(lane & 7), r0 = lane >> 3;
     const unsigned blk = blockIdx.x / (unsigned)a.splits, split = blockIdx.x - blk * (unsigned)a.splits;
@@ -388,7 +398,7 @@ __global__ __launch_bounds__(256, 3) void heads_grad_kernel(HeadsArgs a, HeadsGr
         }
     };
     load(i0 + wave * kItems, 0);
-    if constexpr (ROT != 0) make_table(a, valid, pos_row, table);
+    if constexpr (ROT != 0) make_table(a, valid, [&](int r) { return (long)pos_row[r]; }, table);
     float w[8];
     int have = -1;                                   // tensor whose weights these are
     for (int unit = i0 + wave * kItems; unit < i1; unit += 4 * kItems) {
@@ -418,7 +428,7 @@ __global__ __launch_bounds__(256, 3) void heads_grad_kernel(HeadsArgs a, HeadsGr
                     unpack8(xs[j], u);
                     unpack8(gs[j], n);
                     const float rs = normalise(u, a.norm, a.eps);
-                    if constexpr (ROT != 0) rotate<ROT>(n, table + r * kCsPitch<true>, o, 1);
+                    if constexpr (ROT != 0) rotate<ROT>(n, table + r * kCsPitch, o, 1);
                     if (r < valid) {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) { dw[e] = fmaf(n[e], u[e], dw[e]); db[e] += n[e]; }
