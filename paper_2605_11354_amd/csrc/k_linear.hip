@@ -154,15 +154,23 @@ __global__ __launch_bounds__(256, 2) void fp8_gemm_kernel(const uint8_t *__restr
     constexpr int kStage = (kTok + 128) * kSlice;                                // token groups, then the four channel groups
     __shared__ __attribute__((aligned(1024))) uint8_t smem[3 * kStage + (256 + kTok) * 4 + 16];
     float *const cs = (float *)(smem + 3 * kStage), *const ts = cs + 256, *const red = ts + kTok;    // channel scales, biases; token scales
-    // channel tile fastest: the workgroups that share a token tile run side by side on one XCD, so the activations come
-    // from HBM once; the weight matrix (a few MB) stays in every XCD's L2
+    // channel tile fastest: the workgroups that share a token tile run side by side on one XCD, so the activations come from HBM
+    // once.  Large launches with more than eight channel tiles take eight token tiles through all channel tiles, token tile fastest: the
+    // sixty-four workgroups on an XCD then share eight and eight (2 MB of activations, 1 MB of weights for K = 1024), which its L2 holds; all channels of
+    // one token tile read a weight matrix of 4 MB again for every two token tiles (43968 x 1024 -> 4096: 1.1 GB, as fast as HBM gives it, 241 us with
+    // the quantiser; 219 so.  Eight channel tiles, 43968 x 4096 -> 1024: 309 us, 317 so).
     const int item = (int)xcd_remap(blockIdx.x, total);
     if (item >= total) return;
 #ifdef SLA_PROBE_TIME
     const bool gprobe = __builtin_amdgcn_readfirstlane((int)(item == total / 2 + 5 && threadIdx.x < 64)) != 0;
 #endif
     SLA_GT(0);
-    const int it = (int)((unsigned)item / (unsigned)n_ot), ot = item - it * n_ot;
+    int it = (int)((unsigned)item / (unsigned)n_ot), ot = item - it * n_ot;
+    if (TB == 4 && n_ot > 8) {
+        const int first = (it & ~7), in = item - first * n_ot, rows = min(8, (M + kTok - 1) / kTok - first);
+        ot = (int)((unsigned)in / (unsigned)rows);
+        it = first + in - ot * rows;
+    }
     const int i0 = it * kTok, o0 = ot * 128;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);                  // uniform: LDS destinations of the copies sit in scalar registers
@@ -211,7 +219,7 @@ __global__ __launch_bounds__(256, 2) void fp8_gemm_kernel(const uint8_t *__restr
     // Large launches: workgroups that share an operand tile run at the same time and would ask the same L2 channels for the
     // same lines at the same moment; each starts its K loop at a different step instead.  The sum over K is then taken in a
     // rotated order, which depends on the tile alone and is the same with and without the qkv epilogue.
-    int k2 = TB == 4 ? 2 * (int)((unsigned)item % (unsigned)(ksteps / 2)) : 0;                       // slice that the next issue() copies
+    int k2 = TB == 4 ? 2 * (int)((unsigned)(it * n_ot + ot) % (unsigned)(ksteps / 2)) : 0;                       // slice that the next issue() copies
     auto advance = [&] { k2 = k2 + 1 == ksteps ? 0 : k2 + 1; };
     issue(k2, lds_base);
     advance();
