@@ -4,6 +4,17 @@
 
 namespace sla {
 
+// Row and column of a tile among `cols` tiles to a row of `rows`: along the rows, or, where these are longer than eight, eight rows at a time and
+// down the columns: workgroups that run side by side on an XCD then share rows and columns that its L2 holds.
+struct TileAt { int row, col; };
+__device__ __forceinline__ TileAt tile_at(int item, int rows, int cols)
+{
+    const int row = (int)((unsigned)item / (unsigned)cols);
+    if (cols <= 8) return {row, item - row * cols};
+    const int first = row & ~7, in = item - first * cols, high = min(8, rows - first), col = (int)((unsigned)in / (unsigned)high);
+    return {first + in - col * high, col};
+}
+
 // two copies of 1 KB as copy_1k_to_lds makes them, the second 1 KB behind the first in LDS: four scalar instructions less
 __device__ __forceinline__ void copy_2k_to_lds(const uint8_t *base, uint32_t voff0, uint32_t voff1, uint32_t lds_addr)
 {

@@ -170,7 +170,8 @@ __device__ __forceinline__ void grad_tile(const GradProduct &p, int item, uint8_
     const uint8_t *const B = p.B;
     const int lda = p.lda, M = p.M, cols = p.cols, K = p.K, tiles = p.tiles, n_nt = p.n_nt, k_split = p.k_split;
     float *const part = p.part;
-    const int split = item / tiles, tile = item - split * tiles, mt = tile / n_nt, nt = tile - mt * n_nt;
+    const int split = item / tiles, tile = item - split * tiles;
+    const auto [mt, nt] = tile_at(tile, (M + BM - 1) / BM, n_nt);
     const int m0 = mt * BM, n0 = nt * BN, k0 = split * k_split, k1 = min(K, k0 + k_split);
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = (wave & 1) * 32 * TM, wn = (wave >> 1) * 32 * TN;
@@ -416,8 +417,9 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 // half a round of them is less, and that a sum split less often leaves fewer partials (fp32, written and read again).  Both products
 // take the same, so that one launch has them: where one ends the other fills its CUs (10992 tokens, 1024 -> 1024: 78 us in launches of 256 for
 // dx and of 128 for dW, 70 in one of 128).  256 from 128 such tiles of dx and 100 steps of both products for each CU on:
-//     us, 128 and 256:   43968 tokens, 1024 -> 1024 (172 steps) 231, 225;  10992, 1024 -> 4096 (172) 215, 196;  2048, 4096 -> 4096 (128) 206, 191;
-//     21984, 1024 -> 1024 (86) 119, 133;  5496, 4096 -> 1024 (86) 153, 142;  43968, 384 -> 1152 (73) 102, 134;  4096, 1024 -> 4096 (64) 90, 139
+//     us, 128 and 256:   43968 tokens, 1024 -> 1024 (172 steps) 224, 222;  10992, 1024 -> 4096 (172) 214, 193;  10992, 4096 -> 1024 (172) 226, 216;
+//     2048, 4096 -> 4096 (128) 184, 187;  21984, 1024 -> 1024 (86) 117, 130;  5496, 4096 -> 1024 (86) 130, 139;  43968, 384 -> 1152 (72) 101, 134;
+//     4096, 1024 -> 4096 (64) 88, 136
 //   dx  128 wide: split where there are fewer than 256 tiles (few tokens), into parts of at least eight steps
 //   dW  split into workgroups for the whole chip: 256, or 512 of the small ones, into parts of at least eight steps
 struct Plan {
@@ -428,9 +430,9 @@ struct Plan {
 Plan make_plan(int N, int d_in, int d_out)
 {
     Plan p;
-    const long x256 = tiles_of(N, d_in, 256), w256 = tiles_of(d_out, d_in, 256), x128 = tiles_of(N, d_in, 128), w128 = tiles_of(d_out, d_in, 128);
+    const long w256 = tiles_of(d_out, d_in, 256), x128 = tiles_of(N, d_in, 128), w128 = tiles_of(d_out, d_in, 128);
     const int x_steps = (d_out + kStepK - 1) / kStepK, w_steps = (N + kStepK - 1) / kStepK;
-    p.wide = x256 >= 128 && x256 * x_steps + w256 * w_steps >= 100 * 256;
+    p.wide = tiles_of(N, d_in, 256) >= 128 && 2 * (long)N * d_in / 65536 * d_out / kStepK >= 100 * 256;
     p.splits_x = p.wide || !N ? 1 : even_splits(x_steps, x128 >= 256 ? 1 : std::min(256 / x128, (long)x_steps / 8));
     p.splits_w = even_splits(w_steps, std::min(p.wide ? 256 / w256 : 512 / w128, (long)w_steps / 8));
     p.off_bx = (size_t)((d_out + 31) / 32) * 64 * d_in;

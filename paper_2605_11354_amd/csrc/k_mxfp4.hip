@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void mxfp4_gemm_kernel(const 
     __shared__ __attribute__((aligned(1024))) uint8_t smem[kStages * kStage];
     const int item = (int)xcd_remap(blockIdx.x, total);
     if (item >= total) return;
-    const int it = (int)((unsigned)item / (unsigned)n_ot), ot = item - it * n_ot;
+    const auto [it, ot] = tile_at(item, (M + BM - 1) / BM, n_ot);
     const int i0 = it * BM, o0 = ot * BN;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -429,7 +429,7 @@ bool mxfp4_turns_weights(int M, int O) { return M >= 2L * O; }
 // Tiles.  64 x 128 while each has a CU of its own (256 of them, 2048 x 1024 -> 1024: 6.1 us, 6.7 with 128 x 128; 352, 700 x 1024 -> 4096: 7.5 and
 // 7.0, from 4096 channels 23.3 and 17.0).  A 256 x 256 tile reads half as much from LDS and L2 for a product as four of 128 x 128, but has a CU to
 // itself, with nothing under its start and end: from 192 on (172, 10992 x 1024 -> 1024: 15.2 us and 12.9; 192, 3000 x 1024 -> 4096: 16.0 and 14.0,
-// x 4096: 34.8 and 41.0; 2752, 43968 x 1024 -> 4096: 155 and 158; 688, 43968 x 4096 -> 1024: 102 and 108).
+// x 4096: 34.8 and 41.0; 2752, 43968 x 1024 -> 4096: 150 and 154; 688, 43968 x 4096 -> 1024: 102 and 108).
 hipError_t launch_mxfp4_gemm(const void *A, const void *As, const void *W, const void *Ws, bool by_steps, const void *bias, int M, int O, int K, void *Y, hipStream_t st)
 {
     const long wide = (long)((M + 255) / 256) * ((O + 255) / 256), narrow = (long)((M + 63) / 64) * ((O + 127) / 128);
