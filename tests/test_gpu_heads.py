@@ -255,3 +255,26 @@ def test_tensors_of_another_shape_type_or_place_are_refused():
     h.p.pos_per_item = 1
     with pytest.raises(ValueError, match="pos"):                                             # two items, positions of one
         B.sla_qk_norm_rope(h.p, *h.x, *out, pos=h.pos)
+
+
+@pytest.mark.parametrize("bq", [64, 128])
+def test_e4m3_of_infinities_and_nan_is_the_quantiser_s(bq):
+    """Without norm and rotation q and k are quantised as they are: a block with an infinity (or of NaN alone) comes out as
+    sla_quantise_e4m3 leaves it, v bit for bit, q and k in scales and in which values are finite."""
+    h = Heads(2, 300, 3, norm="none", axes=0)
+    for t in h.x:
+        t[0, 5, 0, 7], t[1, 70, 1, 0], t[1, 299, 2, 63] = float("inf"), float("nan"), float("-inf")
+        t[0, 128:192, 2] = float("nan")
+    codes = [torch.empty((2, 3, 300, 64), dtype=torch.uint8, device="cuda") for _ in range(3)]
+    scales = [torch.empty((2, 3, -(-300 // b)), device="cuda") for b in (bq, 64, 64)]
+    B.sla_qk_norm_rope_e4m3(h.p, *h.x, bq, *codes, *scales)
+    for n, blk in enumerate((bq, 64, 64)):
+        c, s = torch.empty_like(codes[n]), torch.empty_like(scales[n])
+        B.sla_quantise_e4m3(h.x[n].transpose(1, 2).contiguous(), blk, c, s)
+        torch.cuda.synchronize()
+        assert torch.equal(s, scales[n]) and (n < 2 or torch.equal(c, codes[n]))
+        got, want = (t.view(torch.float8_e4m3fn).float() * s.repeat_interleave(blk, 2)[:, :, :300, None] for t in (codes[n], c))
+        assert torch.equal(got.isfinite(), want.isfinite())
+        # a product with 1 / scale instead of the quotient: the neighbouring code where the quotient lies half-way, a step of 2^-3
+        ok = want.isfinite()
+        assert bool(((got - want).abs()[ok] <= 2.0 ** -3 * want.abs()[ok] + 2.0 ** -9 * s.repeat_interleave(blk, 2)[:, :, :300, None].expand_as(want)[ok]).all())
