@@ -417,24 +417,26 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 // half a round of them is less, and that a sum split less often leaves fewer partials (fp32, written and read again).  Both products
 // take the same, so that one launch has them: where one ends the other fills its CUs (10992 tokens, 1024 -> 1024: 78 us in launches of 256 for
 // dx and of 128 for dW, 70 in one of 128).  256 from 128 such tiles of dx and 100 steps of both products for each CU on:
-//     us, 128 and 256:   43968 tokens, 1024 -> 1024 (172 steps) 224, 222;  10992, 1024 -> 4096 (172) 214, 193;  10992, 4096 -> 1024 (172) 226, 216;
-//     2048, 4096 -> 4096 (128) 184, 187;  21984, 1024 -> 1024 (86) 117, 130;  5496, 4096 -> 1024 (86) 130, 139;  43968, 384 -> 1152 (72) 101, 134;
-//     4096, 1024 -> 4096 (64) 88, 136
+//     us, 128 and 256:   43968 tokens, 1024 -> 1024 (172 steps) 224, 212;  10992, 1024 -> 4096 (172) 210, 199;  10992, 4096 -> 1024 (172) 226, 212;
+//     2048, 4096 -> 4096 (128) 184, 187;  21984, 1024 -> 1024 (86) 116, 130;  5496, 4096 -> 1024 (86) 120, 139;  43968, 384 -> 1152 (72) 100, 134;
+//     4096, 1024 -> 4096 (64) 85, 136
 //   dx  128 wide: split where there are fewer than 256 tiles (few tokens), into parts of at least eight steps
-//   dW  split into workgroups for the whole chip: 256, or 512 of the small ones, into parts of at least eight steps
+//   dW  split into parts of at least eight steps: beside dx, which has as much work, for half of the places (128 or, small, 256 workgroups), alone
+//       for all of them.  us, all and half: 1374, 1024 -> 4096 54 and 43;  10992, 1024 -> 1024 72 and 67;  10992, 384 -> 1152 44 and 38;
+//       43968, 1024 -> 1024 227 and 212;  43968, 1024 -> 4096 672 and 657;  10992, 1024 -> 4096 193 and 199
 struct Plan {
     bool wide;
     int splits_x, splits_w;
     size_t off_bx, off_part_x, off_part_w, off_part_db, total;                   // the operand of dx comes first
 };
-Plan make_plan(int N, int d_in, int d_out)
+Plan make_plan(int N, int d_in, int d_out, bool both)
 {
     Plan p;
     const long w256 = tiles_of(d_out, d_in, 256), x128 = tiles_of(N, d_in, 128), w128 = tiles_of(d_out, d_in, 128);
     const int x_steps = (d_out + kStepK - 1) / kStepK, w_steps = (N + kStepK - 1) / kStepK;
     p.wide = tiles_of(N, d_in, 256) >= 128 && 2 * (long)N * d_in / 65536 * d_out / kStepK >= 100 * 256;
     p.splits_x = p.wide || !N ? 1 : even_splits(x_steps, x128 >= 256 ? 1 : std::min(256 / x128, (long)x_steps / 8));
-    p.splits_w = even_splits(w_steps, std::min(p.wide ? 256 / w256 : 512 / w128, (long)w_steps / 8));
+    p.splits_w = even_splits(w_steps, std::min((both ? 1 : 2) * (p.wide ? 128 : 256) / (p.wide ? w256 : w128), (long)w_steps / 8));
     p.off_bx = (size_t)((d_out + 31) / 32) * 64 * d_in;
     p.off_part_x = p.off_bx + (size_t)((N + 31) / 32) * 64 * d_in;
     p.off_part_w = p.off_part_x + (p.splits_x > 1 ? up256((size_t)p.splits_x * N * d_in * 4) : 0);
@@ -462,12 +464,12 @@ hipError_t launch_products(bool wide, const GradProduct &w, const GradProduct &x
 }
 }  // namespace
 
-size_t linear_grad_workspace(int N, int d_in, int d_out) { return make_plan(N, d_in, d_out).total; }
+size_t linear_grad_workspace(int N, int d_in, int d_out) { return std::max(make_plan(N, d_in, d_out, true).total, make_plan(N, d_in, d_out, false).total); }
 
 hipError_t launch_linear_grad(const void *dy, const void *x8, const float *sx, const void *W, int N, int d_in, int d_out, void *dx, void *dW, void *db,
                               void *workspace, hipStream_t st)
 {
-    const Plan p = make_plan(N, d_in, d_out);
+    const Plan p = make_plan(N, d_in, d_out, dx && dW);
     char *const ws = (char *)workspace;
     GradSums sums = {};
     auto add = [&](int i, const float *part, void *out, long count, int splits) {
