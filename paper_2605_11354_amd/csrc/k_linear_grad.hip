@@ -260,9 +260,9 @@ __device__ __forceinline__ void grad_tile(const GradProduct &p, int item, uint8_
             }
         }
     };
-    // the next stage is whole and everybody is done with the one before it; AHEAD: later steps whose copies may still be under way
+    // the next stage is whole and everybody is done with the one before it; AHEAD: copies of later steps, which may still be under way
     auto change = [&](auto ahead) {
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(ahead)::value * kCopies) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(ahead)::value) : "memory");
         lds_barrier();
     };
     auto change_to_last = [&](int stage) {           // and what of it lies past K is cleared
@@ -272,15 +272,19 @@ __device__ __forceinline__ void grad_tile(const GradProduct &p, int item, uint8_
             lds_barrier();
         }
     };
-    constexpr int kOperands = TM + TN, kEvery = TM * TN / kCopies > 0 ? TM * TN / kCopies : 1;
+    // half of the copies behind the last products of either part, every second one: the first have the reads behind them, and the six
+    // instructions of a copy fill a gap (all in the first part: 43968 tokens, 1024 -> 4096 646 us, so 634)
+    constexpr int kOperands = TM + TN, kHalf = kCopies / 2, kFirst = TM * TN - 2 * kHalf;
+    auto copy_behind = [&](int i, int k, int half) {
+        if (i >= kFirst && (i - kFirst) % 2 == 0) copy_one(k, half * kHalf + (i - kFirst) / 2);
+    };
     auto step = [&](int s, auto copies, auto ahead, auto last) {
         constexpr bool kCopy = decltype(copies)::value, kLast = decltype(last)::value;
         const int k3 = k0 + (s + 3) * kStepK;
         if constexpr (kCopy) aim(k3, (s + 3) & 3);
         multiply(0, [&](int i) {
             if (i < kOperands) read_one(1, s & 3, 1, i);
-            if constexpr (kCopy)
-                if (i % kEvery == 0 && i / kEvery < kCopies) copy_one(k3, i / kEvery);
+            if constexpr (kCopy) copy_behind(i, k3, 0);
         });
         if constexpr (!kLast) {
             change(ahead);
@@ -289,12 +293,14 @@ __device__ __forceinline__ void grad_tile(const GradProduct &p, int item, uint8_
         multiply(1, [&](int i) {
             if constexpr (!kLast)
                 if (i < kOperands) read_one(0, (s + 1) & 3, 0, i);
+            if constexpr (kCopy) copy_behind(i, k3, 1);
         });
     };
-    static_assert(kOperands <= TM * TN && kCopies * kEvery <= TM * TN, "a part has room for its reads and copies");
+    static_assert(kOperands <= TM * TN && kCopies % 2 == 0 && kFirst >= 0, "a part has room for its reads and copies");
     using Ahead0 = std::integral_constant<int, 0>;
-    using Ahead1 = std::integral_constant<int, 1>;
-    using Ahead2 = std::integral_constant<int, 2>;
+    using Ahead1 = std::integral_constant<int, kCopies>;
+    using Ahead2 = std::integral_constant<int, 2 * kCopies>;
+    using InLoop = std::integral_constant<int, 2 * kCopies - kHalf>;             // the second half of step s + 3 is asked for behind the barrier
     using Yes = std::true_type;
     using No = std::false_type;
 
@@ -311,7 +317,7 @@ __device__ __forceinline__ void grad_tile(const GradProduct &p, int item, uint8_
 #pragma unroll
     for (int x = 0; x < kOperands; ++x) read_one(0, 0, 0, x);
     int s = 0;
-    for (; s + 3 < steps; ++s) step(s, Yes{}, Ahead2{}, No{});
+    for (; s + 3 < steps; ++s) step(s, Yes{}, InLoop{}, No{});
     if (s + 2 < steps) step(s++, No{}, Ahead1{}, No{});
     if (s + 1 < steps) step(s++, No{}, Ahead0{}, No{});
     step(s, No{}, Ahead0{}, Yes{});
