@@ -160,7 +160,8 @@ struct GradProduct {
 // steps ago), and its first operands are read under those products.
 // With TM = TN = 4 a wave holds 256 accumulators and a CU one workgroup: a part takes 8 operands per 16 matrix instructions from
 // LDS, half of what its bandwidth allows (128 x 64 per wave: three quarters, with the writes all of it).
-// Measured: both products of 43968 tokens, 1024 -> 4096 615 to 690 us (1.07 to 1.2 PFLOP/s: the clock that the chip grants); as library products 358 and 559.
+// Measured: both products of 43968 tokens, 1024 -> 4096 590 to 640 us (1.15 to 1.25 PFLOP/s: the clock that the chip grants); as library products 358 and 559.
+// The matrix unit is busy 72 % of the cycles in which a CU has work; with all copies from the L2 a tenth less time, with a fifth stage the same.
 template <int TM, int TN, bool TURN>
 __device__ __forceinline__ void grad_tile(const GradProduct &p, int item, uint8_t *smem)
 {
@@ -272,11 +273,12 @@ __device__ __forceinline__ void grad_tile(const GradProduct &p, int item, uint8_
             lds_barrier();
         }
     };
-    // half of the copies behind the last products of either part, every second one: the first have the reads behind them, and the six
-    // instructions of a copy fill a gap (all in the first part: 43968 tokens, 1024 -> 4096 646 us, so 634)
-    constexpr int kOperands = TM + TN, kHalf = kCopies / 2, kFirst = TM * TN - 2 * kHalf;
-    auto copy_behind = [&](int i, int k, int half) {
-        if (i >= kFirst && (i - kFirst) % 2 == 0) copy_one(k, half * kHalf + (i - kFirst) / 2);
+    // 256 x 256: half of the copies behind the last products of either part, every second one: the first have the reads behind them, and the six
+    // instructions of a copy fill a gap (all in the first part: 43968 tokens, 1024 -> 4096 646 us, so 634).  128 x 128, where another workgroup
+    // fills the gaps: all behind the first part's, the sooner the better (10992 tokens, 1024 -> 1024, the whole step 107.7 us, halves 109.8)
+    constexpr int kOperands = TM + TN, kSecond = TM == 4 ? kCopies / 2 : 0, kGap = TM == 4 ? 2 : 1, kFirst = TM * TN - (kCopies - kSecond) * kGap;
+    auto copy_behind = [&](int i, int k, int done, int count) {
+        if (i >= kFirst && (i - kFirst) % kGap == 0 && (i - kFirst) / kGap < count) copy_one(k, done + (i - kFirst) / kGap);
     };
     auto step = [&](int s, auto copies, auto ahead, auto last) {
         constexpr bool kCopy = decltype(copies)::value, kLast = decltype(last)::value;
@@ -284,7 +286,7 @@ __device__ __forceinline__ void grad_tile(const GradProduct &p, int item, uint8_
         if constexpr (kCopy) aim(k3, (s + 3) & 3);
         multiply(0, [&](int i) {
             if (i < kOperands) read_one(1, s & 3, 1, i);
-            if constexpr (kCopy) copy_behind(i, k3, 0);
+            if constexpr (kCopy) copy_behind(i, k3, 0, kCopies - kSecond);
         });
         if constexpr (!kLast) {
             change(ahead);
@@ -293,14 +295,14 @@ __device__ __forceinline__ void grad_tile(const GradProduct &p, int item, uint8_
         multiply(1, [&](int i) {
             if constexpr (!kLast)
                 if (i < kOperands) read_one(0, (s + 1) & 3, 0, i);
-            if constexpr (kCopy) copy_behind(i, k3, 1);
+            if constexpr (kCopy) copy_behind(i, k3, kCopies - kSecond, kSecond);
         });
     };
     static_assert(kOperands <= TM * TN && kCopies % 2 == 0 && kFirst >= 0, "a part has room for its reads and copies");
     using Ahead0 = std::integral_constant<int, 0>;
     using Ahead1 = std::integral_constant<int, kCopies>;
     using Ahead2 = std::integral_constant<int, 2 * kCopies>;
-    using InLoop = std::integral_constant<int, 2 * kCopies - kHalf>;             // the second half of step s + 3 is asked for behind the barrier
+    using InLoop = std::integral_constant<int, 2 * kCopies - kSecond>;           // those of step s + 3's are asked for behind the barrier
     using Yes = std::true_type;
     using No = std::false_type;
 
