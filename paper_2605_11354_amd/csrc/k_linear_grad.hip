@@ -161,7 +161,7 @@ struct GradProduct {
 // With TM = TN = 4 a wave holds 256 accumulators and a CU one workgroup: a part takes 8 operands per 16 matrix instructions from
 // LDS, half of what its bandwidth allows (128 x 64 per wave: three quarters, with the writes all of it).
 // Measured: both products of 43968 tokens, 1024 -> 4096 590 to 640 us (1.15 to 1.25 PFLOP/s: the clock that the chip grants); as library products 358 and 559.
-// The matrix unit is busy 72 % of the cycles in which a CU has work; with all copies from the L2 a tenth less time, with a fifth stage the same.
+// The matrix unit is busy 78 % of the cycles in which a CU has work; with all copies from the L2 a tenth less time, with a fifth stage the same.
 template <int TM, int TN, bool TURN>
 __device__ __forceinline__ void grad_tile(const GradProduct &p, int item, uint8_t *smem)
 {
@@ -369,7 +369,7 @@ __global__ __launch_bounds__(256, T == 4 ? 1 : 2) void linear_grad_kernel(GradPr
     }
 }
 
-// HBM bound: four splits of 4096 x 1024 16 us (75 MB, 4.7 TB/s).  out[i] = bf16(sum of the splits' partials, in order), for up to three outputs; counts are multiples of 8
+// HBM bound: four splits of 1024 x 1024 4 to 5 us, two of 4096 x 1024 8 us (42 MB, 5 TB/s).  out[i] = bf16(sum of the splits' partials, in order), for up to three outputs; counts are multiples of 8
 struct GradSums {
     const float *part[3];
     uint16_t *out[3];
