@@ -126,3 +126,45 @@ def test_training_layer(Bn, N, H, per_head):
     rx, rW, rb = po.fp8_linear_backward(xb, Wb, d.reshape(T, -1))
     for got, ref in ((dx, rx), (dW, rW), (db, rb)):
         assert np.linalg.norm(f64(got) - ref) <= 9.4e-3 * np.linalg.norm(ref)
+
+
+def test_calls_at_once_on_two_streams():
+    """Two layers on two streams, each with workspaces of its own: the bits of one after the other."""
+    def make(seed, N, d_in, H):
+        g, xb, Wb, bb = draw(seed, N, d_in, 3 * H * 64)
+        t = dict(x=G.dev_bf16(xb), W=G.dev_bf16(Wb), b=G.dev_bf16(bb), N=N, H=H, d_in=d_in, d_out=3 * H * 64)
+        bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16, device="cuda")
+        u8 = lambda *s: torch.zeros(s, dtype=torch.uint8, device="cuda")
+        t.update(y=bf(N, t["d_out"]), ck=u8(B.sla_fp8_checkpoint_bytes(N, d_in)), ws=u8(B.sla_fp8_linear_grad_workspace_bytes(N, d_in, t["d_out"])),
+                 dx=bf(N, d_in), dW=bf(t["d_out"], d_in), db=bf(t["d_out"]), Wc=u8(t["d_out"], d_in // 2), Ws=u8(t["d_out"], d_in // 32), y4=bf(N, t["d_out"]),
+                 mws=u8(max(256, B.sla_mxfp4_linear_workspace_bytes(N, d_in, t["d_out"]))), out=[bf(1, H, N, 64) for _ in range(3)], d=bf(N, t["d_out"]),
+                 dw=[torch.zeros(64, device="cuda") for _ in range(4)])
+        t["p"] = B.make_heads_params(t["y"].view(1, N, 3, H, 64)[:, :, 0], axes=0)
+        t["hws"] = u8(max(256, B.sla_qk_norm_rope_grad_workspace_bytes(t["p"])))
+        return t
+
+    def layer(t):
+        B.sla_fp8_linear_save(t["x"], t["W"], t["b"], t["y"], t["ck"], t["ws"])
+        q, k, v = t["y"].view(1, t["N"], 3, t["H"], 64).unbind(2)
+        B.sla_qk_norm_rope(t["p"], q, k, v, *t["out"])
+        d = t["d"].view(1, t["N"], 3, t["H"], 64).unbind(2)
+        B.sla_qk_norm_rope_grad(t["p"], q, k, *t["out"], *d, dq_weight=t["dw"][0], dq_bias=t["dw"][1], dk_weight=t["dw"][2], dk_bias=t["dw"][3], workspace=t["hws"])
+        B.sla_fp8_linear_grad(t["d"], t["ck"], t["W"], t["dx"], t["dW"], t["db"], t["ws"])
+        B.sla_quantise_mxfp4(t["W"], t["Wc"], t["Ws"])
+        B.sla_mxfp4_linear(t["x"], t["Wc"], t["Ws"], t["b"], t["y4"], t["mws"])
+        return [t["y"], *t["out"], t["d"], *t["dw"], t["dx"], t["dW"], t["db"], t["y4"]]
+
+    layers = make(1, 1500, 384, 4), make(2, 700, 512, 6)
+    want = [[o.clone() for o in layer(t)] for t in layers]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = []
+        for t, s in zip(layers, streams):
+            with torch.cuda.stream(s):
+                for name in ("y", "dx", "dW", "db", "y4", "d"):
+                    t[name].zero_()
+                got.append(layer(t))
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a, b))
