@@ -92,7 +92,7 @@ CASES = [
     dict(Bn=5, N=37, H=7, axes=1, base=1e4, kind="head_major", far=100000), dict(Bn=2, N=129, H=2, axes=2, pairing="adjacent", layout="bnhd", pad=8),
     dict(Bn=1, N=200, H=3, norm="none", axes=2), dict(Bn=1, N=130, H=12, norm="layer", axes=0, per_head=True), dict(Bn=1, N=70, H=2, norm="none", axes=0),
     dict(Bn=1, N=4500, H=16, kind="per_head"), dict(Bn=70, N=2, H=1, axes=1, own_pos=True), dict(Bn=2, N=100, H=6, weights=False),
-    dict(Bn=3, N=75, H=2, kind="token_first"),
+    dict(Bn=3, N=75, H=2, kind="token_first"), dict(Bn=3, N=11003, H=2), dict(Bn=1, N=33001, H=1, norm="rms", axes=1, pairing="adjacent", base=1e4, layout="bnhd"),
 ]
 
 
