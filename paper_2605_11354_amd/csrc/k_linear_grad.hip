@@ -97,7 +97,10 @@ __global__ __launch_bounds__(256) void grad_operands_kernel(const uint16_t *__re
         const int R = min(32, d_out - 32 * grp);
         const uint16_t *const from = W + (size_t)32 * grp * cols;
         float top[4] = {0.f, 0.f, 0.f, 0.f};         // of rows lane / 8 + 8 i, over 64 columns at a time
-        for (int s = wave; s < cols / 64; s += 4)
+        const int n = cols / 64, turn = (int)(blockIdx.x % (unsigned)n);          // workgroups begin at columns, and so channels of the L2, of their own
+#pragma unroll 4
+        for (int s0 = wave; s0 < n; s0 += 4) {
+            const int s = s0 + turn < n ? s0 + turn : s0 + turn - n;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint4 u = *(const uint4 *)(from + (size_t)min((lane >> 3) + 8 * i, R - 1) * cols + 64 * s + 8 * (lane & 7));
@@ -105,10 +108,13 @@ __global__ __launch_bounds__(256) void grad_operands_kernel(const uint16_t *__re
 #pragma unroll
                 for (int q = 0; q < 4; ++q) top[i] = fmaxf(top[i], fmaxf(fabsf(bf16_lo(w[q])), fabsf(bf16_hi(w[q]))));
             }
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-#pragma unroll
-            for (int x = 1; x < 8; x <<= 1) top[i] = fmaxf(top[i], __shfl_xor(top[i], x, 64));
+            // over eight lanes
+            top[i] = fmaxf(top[i], __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(top[i]), 0xB1, 0xf, 0xf, true)));
+            top[i] = fmaxf(top[i], __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(top[i]), 0x4E, 0xf, 0xf, true)));
+            top[i] = fmaxf(top[i], __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(top[i]), 0x141, 0xf, 0xf, true)));
             if ((lane & 7) == 0) red[wave][(lane >> 3) + 8 * i] = top[i];
         }
         __syncthreads();
