@@ -243,7 +243,8 @@ sla_status_t sla_dequantise_mxfp4(const void *codes, const void *scales, int64_t
 
 /*
  * Linear layer with weights in that form, for serving: x is quantised as sla_quantise_mxfp4 does, then y = x4 W4^T + bias with
- * exact products, fp32 sums and one rounding to bf16.  At most 32 tokens (a decoding step) take one launch and no workspace.
+ * exact products, fp32 sums and one rounding to bf16.  At most 32 tokens (a decoding step), and
+ * up to 64 where that is quicker, take one launch and no workspace (sla_mxfp4_linear_workspace_bytes says 0).
  *   x      in   bf16 [N, d_in]                      d_in a multiple of 128
  *   W      in   codes uint8 [d_out, d_in/2] and scales uint8 [d_out, d_in/32]      d_out a multiple of 8
  *   bias   in   bf16 [d_out] or NULL

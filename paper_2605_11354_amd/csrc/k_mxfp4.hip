@@ -387,9 +387,11 @@ hipError_t launch_dequantise_mxfp4(const void *codes, const void *scales, long r
     return hipGetLastError();
 }
 
-// One launch while quantising x in every workgroup costs less than a launch of its own: 32 tokens through 4096 x 4096 8.9 us (12.7 with two launches),
-// 1024 x 1024 4.1 (6.9), 1152 -> 8208 7.3 (7.1); every four tokens more cost 0.8, 0.2 and 0.7 us here and nothing there.
-bool mxfp4_few(int M) { return M <= 32; }
+// One launch while quantising x in every workgroup costs less than a launch of its own: 32 tokens through 4096 x 4096 8.9 us (13.0 with two launches),
+// 1024 x 1024 4.1 (6.9), 4096 -> 8192 12.9 (12.8); up to 64 where four or eight waves share K, none has much of it, and each workgroup has a CU of its own: 48 tokens
+// through 1024 x 1024 4.9 (7.0), 64 tokens 5.7 (7.0), 2048 x 2048 8.1 (8.7), but 4096 x 4096 14.6 (13.3), 128 -> 1024 7.6 (5.4),
+// 2048 -> 8192 16.6 (8.9).
+bool mxfp4_few(int M, int O, int K) { return M <= 32 || (M <= 64 && K >= 512 && O <= 4096 && (M + 15) / 16 * ((K + 1023) / 1024) <= 12); }
 
 namespace {
 template <int Q> hipError_t launch_few(const void *X, const void *W, const void *Ws, const void *bias, int M, int O, int K, void *Y, hipStream_t st)
@@ -418,7 +420,9 @@ hipError_t launch_mxfp4_few(const void *X, const void *W, const void *Ws, const 
     if (M <= 4) return launch_few<1>(X, W, Ws, bias, M, O, K, Y, st);
     if (M <= 8) return launch_few<2>(X, W, Ws, bias, M, O, K, Y, st);
     if (M <= 16) return launch_few<4>(X, W, Ws, bias, M, O, K, Y, st);
-    return launch_few<8>(X, W, Ws, bias, M, O, K, Y, st);
+    if (M <= 32) return launch_few<8>(X, W, Ws, bias, M, O, K, Y, st);
+    if (M <= 48) return launch_few<12>(X, W, Ws, bias, M, O, K, Y, st);
+    return launch_few<16>(X, W, Ws, bias, M, O, K, Y, st);
 }
 
 // W by steps costs its quantiser launch (17/32 O K bytes read and written): where both products take as long as that, with M = O

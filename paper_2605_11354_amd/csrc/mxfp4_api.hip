@@ -29,7 +29,7 @@ sla_status_t make_mx_plan(int32_t N, int32_t d_in, int32_t d_out, MxPlan &mp)
     mp.off_scales = align_up((size_t)N, 16) * d_in / 2;
     mp.off_w = mp.off_scales + align_up((size_t)N * d_in / 32, 256);
     mp.off_ws = mp.off_w + (turned ? align_up((size_t)d_out, 16) * d_in / 2 : 0);
-    mp.total = sla::mxfp4_few(N) ? 0 : mp.off_ws + (turned ? align_up((size_t)d_out * d_in / 32, 256) : 0);
+    mp.total = sla::mxfp4_few(N, d_out, d_in) ? 0 : mp.off_ws + (turned ? align_up((size_t)d_out * d_in / 32, 256) : 0);
     return SLA_OK;
 }
 
@@ -74,7 +74,7 @@ sla_status_t sla_mxfp4_linear(const void *x, const void *W_codes, const void *W_
     SLA_REQ_PTR(x); SLA_REQ_PTR(W_codes); SLA_REQ_PTR(W_scales); SLA_REQ_PTR(y);
     SLA_OPT_PTR(bias);
     hipStream_t st = (hipStream_t)stream;
-    if (sla::mxfp4_few(N)) {
+    if (sla::mxfp4_few(N, d_out, d_in)) {
         SLA_HIP(sla::launch_mxfp4_few(x, W_codes, W_scales, bias, N, d_out, d_in, y, st));
         return SLA_OK;
     }

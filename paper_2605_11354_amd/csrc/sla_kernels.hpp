@@ -110,7 +110,7 @@ bool mxfp4_turns_weights(int M, int O);            // whether a product with M t
 // Y bf16 [M,O] = A [M,K] W [O,K]^T + bias: A, As by steps, W, Ws by steps or as they lie, K a multiple of 128, O of 8; bias may be NULL
 hipError_t launch_mxfp4_gemm(const void *A, const void *As, const void *W, const void *Ws, bool by_steps, const void *bias, int M, int O, int K, void *Y, hipStream_t st);
 // the same for few rows of bf16 X, quantised on the way (no workspace)
-bool mxfp4_few(int M);
+bool mxfp4_few(int M, int O, int K);
 hipError_t launch_mxfp4_few(const void *X, const void *W, const void *Ws, const void *bias, int M, int O, int K, void *Y, hipStream_t st);
 
 // Norm and rotation of the heads of a projection's output (k_heads.hip).  Strides in elements; x and y [0..2] = q, k, v.

@@ -72,7 +72,7 @@ def layer(N, d_in, d_out, seed=0):
     return x, W, synth.to_bf16_bits(g.standard_normal(d_out).astype(np.float32))
 
 
-SIZES = [(1, 128, 8), (1, 4096, 520), (2, 256, 4096), (4, 640, 40), (5, 384, 264), (8, 1024, 24), (9, 128, 520), (15, 384, 136), (16, 1152, 16), (17, 128, 8200), (32, 2048, 264), (33, 128, 8), (64, 256, 72),
+SIZES = [(1, 128, 8), (1, 4096, 520), (2, 256, 4096), (4, 640, 40), (5, 384, 264), (8, 1024, 24), (9, 128, 520), (15, 384, 136), (16, 1152, 16), (17, 128, 8200), (32, 2048, 264), (33, 128, 8), (64, 256, 72), (33, 512, 264), (48, 1024, 72), (49, 640, 520), (64, 2048, 4096), (60, 1024, 4104),
          (65, 384, 136), (197, 640, 1160), (1000, 128, 64), (2049, 256, 3080), (6500, 128, 1024), (8195, 384, 2056), (4100, 256, 4360)]
 
 
