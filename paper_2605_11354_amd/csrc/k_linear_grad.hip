@@ -434,10 +434,13 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 //     us, 128 and 256:   43968 tokens, 1024 -> 1024 (172 steps) 224, 212;  10992, 1024 -> 4096 (172) 210, 199;  10992, 4096 -> 1024 (172) 226, 212;
 //     2048, 4096 -> 4096 (128) 184, 187;  21984, 1024 -> 1024 (86) 116, 130;  5496, 4096 -> 1024 (86) 120, 139;  43968, 384 -> 1152 (72) 100, 134;
 //     4096, 1024 -> 4096 (64) 85, 136
-//   dx  128 wide: split where there are fewer than 256 tiles (few tokens), into parts of at least eight steps
-//   dW  split into parts of at least eight steps: beside dx, which has as much work, for half of the places (128 or, small, 256 workgroups), alone
-//       for all of them.  us, all and half: 1374, 1024 -> 4096 54 and 43;  10992, 1024 -> 1024 72 and 67;  10992, 384 -> 1152 44 and 38;
-//       43968, 1024 -> 1024 227 and 212;  43968, 1024 -> 4096 672 and 657;  10992, 1024 -> 4096 193 and 199
+//   dW  split into parts of at least twenty steps: beside dx, which has as much work, for half of the places (128 or, small, 256 workgroups),
+//       alone for all of them.  us, all and half: 1374, 1024 -> 4096 54 and 43;  10992, 1024 -> 1024 72 and 67;  10992, 384 -> 1152 44 and 38;
+//       43968, 1024 -> 1024 227 and 212;  43968, 1024 -> 4096 672 and 657;  10992, 1024 -> 4096 193 and 199.  Parts of eight and of twenty:
+//       700, 1024 -> 1024 23.5 and 19.4;  1374, 384 -> 1152 22.7 and 20.5
+//   dx  128 wide, fewer than 256 tiles: split into parts as long as those of dW and at least eight steps, where what that saves (0.27 us a step) is more than
+//       the launch and the partials of the sum cost.  us, split and whole: 197, 1024 -> 4096 24 and 43;  197, 384 -> 1152 13.2 and 15.4;
+//       197, 128 -> 512 11.8 and 10.3;  394, 1024 -> 1024 19.9 and 17.8;  1374, 384 -> 1152 26.2 and 22.7;  197, 4096 -> 1024 36 and 30
 struct Plan {
     bool wide;
     int splits_x, splits_w;
@@ -449,8 +452,12 @@ Plan make_plan(int N, int d_in, int d_out, bool both)
     const long w256 = tiles_of(d_out, d_in, 256), x128 = tiles_of(N, d_in, 128), w128 = tiles_of(d_out, d_in, 128);
     const int x_steps = (d_out + kStepK - 1) / kStepK, w_steps = (N + kStepK - 1) / kStepK;
     p.wide = tiles_of(N, d_in, 256) >= 128 && 2 * (long)N * d_in / 65536 * d_out / kStepK >= 100 * 256;
-    p.splits_x = p.wide || !N ? 1 : even_splits(x_steps, x128 >= 256 ? 1 : std::min(256 / x128, (long)x_steps / 8));
-    p.splits_w = even_splits(w_steps, std::min((both ? 1 : 2) * (p.wide ? 128 : 256) / (p.wide ? w256 : w128), (long)w_steps / 8));
+    p.splits_w = even_splits(w_steps, std::min((both ? 1 : 2) * (p.wide ? 128 : 256) / (p.wide ? w256 : w128), (long)w_steps / 20));
+    p.splits_x = 1;
+    if (!p.wide && N && x128 < 256) {
+        const int part = std::max(8, (w_steps + p.splits_w - 1) / p.splits_w), splits = even_splits(x_steps, std::min(256 / x128, (long)x_steps / part));
+        if (0.27 * (x_steps - x_steps / splits) > 2.5 + 0.028 * x128 * splits) p.splits_x = splits;
+    }
     p.off_bx = (size_t)((d_out + 31) / 32) * 64 * d_in;
     p.off_part_x = p.off_bx + (size_t)((N + 31) / 32) * 64 * d_in;
     p.off_part_w = p.off_part_x + (p.splits_x > 1 ? up256((size_t)p.splits_x * N * d_in * 4) : 0);
