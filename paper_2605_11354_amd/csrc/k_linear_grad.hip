@@ -81,9 +81,9 @@ __device__ __forceinline__ void turn_tile(const i32x4 (&c)[4], float scale, uint
 }
 
 // Both products' B in one launch.  The first w_blocks workgroups quantise W (bf16 [d_out, cols]) as the layer's forward does and turn
-// the numbers at once: a workgroup takes 32 rows and 512 columns, for which it needs the maxima of the whole rows.  The others turn the
-// kept codes of x: 32 rows and 128 columns a wave.  HBM bound: 43968 tokens, 1024 -> 4096 28 us (45 MB of codes in, 90 MB out, and W: 5.2 TB/s).
-__global__ __launch_bounds__(256) void grad_operands_kernel(const uint16_t *__restrict__ W, int d_out, uint8_t *__restrict__ Bw, unsigned w_blocks,
+// the numbers at once: `parts` workgroups share 32 rows, 128 columns at a time for each of their waves, and each needs the maxima of the whole
+// rows.  The others turn the kept codes of x: 32 rows and 128 columns a wave.  HBM bound: 43968 tokens, 1024 -> 4096 28 us (45 MB of codes in, 90 MB out, and W: 5.2 TB/s).
+__global__ __launch_bounds__(256) void grad_operands_kernel(const uint16_t *__restrict__ W, int d_out, uint8_t *__restrict__ Bw, unsigned w_blocks, unsigned parts,
                                                             const uint8_t *__restrict__ codes, const float *__restrict__ scales, int rows,
                                                             uint8_t *__restrict__ Bx, int cols)
 {
@@ -93,7 +93,7 @@ __global__ __launch_bounds__(256) void grad_operands_kernel(const uint16_t *__re
     const int spans = cols / 128;
     i32x4 c[4];
     if (blockIdx.x < w_blocks) {
-        const int parts = (spans + 3) / 4, grp = (int)(blockIdx.x / (unsigned)parts), span = (int)(blockIdx.x - grp * (unsigned)parts) * 4 + wave;
+        const int grp = (int)(blockIdx.x / parts), part = (int)(blockIdx.x - grp * parts);
         const int R = min(32, d_out - 32 * grp);
         const uint16_t *const from = W + (size_t)32 * grp * cols;
         float top[4] = {0.f, 0.f, 0.f, 0.f};         // of rows lane / 8 + 8 i, over 64 columns at a time
@@ -118,20 +118,22 @@ __global__ __launch_bounds__(256) void grad_operands_kernel(const uint16_t *__re
             if ((lane & 7) == 0) red[wave][(lane >> 3) + 8 * i] = top[i];
         }
         __syncthreads();
-        if (span >= spans) return;                   // nothing below synchronises across waves
         const float scale = training_scale(fmaxf(fmaxf(red[0][r], red[1][r]), fmaxf(red[2][r], red[3][r])));
         const BlockDivisor divide(scale);
+        for (int span = part * 4 + wave; span < spans; span += 4 * (int)parts) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const int run = (x & 1) * 2 + (lane >> 5), col = 16 * (4 * (x >> 1) + 2 * (run & 1) + (run >> 1));
-            const uint16_t *const at = from + (size_t)min(r, R - 1) * cols + 128 * span + col;
-            const uint4 u = *(const uint4 *)at, v = *(const uint4 *)(at + 8);
-            const uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
-            c[x] = __builtin_bit_cast(i32x4, quantise16(w, divide));
+            for (int x = 0; x < 4; ++x) {
+                const int run = (x & 1) * 2 + (lane >> 5), col = 16 * (4 * (x >> 1) + 2 * (run & 1) + (run >> 1));
+                const uint16_t *const at = from + (size_t)min(r, R - 1) * cols + 128 * span + col;
+                const uint4 u = *(const uint4 *)at, v = *(const uint4 *)(at + 8);
+                const uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+                c[x] = __builtin_bit_cast(i32x4, quantise16(w, divide));
+            }
+            // rows that are not there: zeros, of finite scale
+            if (r >= R) for (int x = 0; x < 4; ++x) c[x] = i32x4{0, 0, 0, 0};
+            turn_tile(c, r < R ? scale : 0.f, smem + wave * 8192, lane, span, grp, (d_out + 31) / 32, Bw);
+            wave_lds_sync();                         // the tile has been read
         }
-        // rows that are not there: zeros, of finite scale
-        if (r >= R) for (int x = 0; x < 4; ++x) c[x] = i32x4{0, 0, 0, 0};
-        turn_tile(c, r < R ? scale : 0.f, smem + wave * 8192, lane, span, grp, (d_out + 31) / 32, Bw);
     } else {
         const int groups = (rows + 31) / 32;
         const long at = (long)(blockIdx.x - w_blocks) * 4 + wave;
@@ -499,9 +501,11 @@ hipError_t launch_linear_grad(const void *dy, const void *x8, const float *sx, c
     if (N > 0) {
         uint8_t *const bw = (uint8_t *)ws, *const bx = (uint8_t *)ws + p.off_bx;
         const int spans = d_in / 128;
-        const long w_blocks = dx ? (long)((d_out + 31) / 32) * ((spans + 3) / 4) : 0, x_blocks = dW ? ((long)((N + 31) / 32) * spans + 3) / 4 : 0;
+        // parts: workgroups for the whole chip, no more, since each reads all of its rows (4096 x 4096: two for each 32 rows 24 us, eight 54)
+        const int w_groups = (d_out + 31) / 32, parts = std::max(1, std::min(256 / w_groups, (spans + 3) / 4));
+        const long w_blocks = dx ? (long)w_groups * parts : 0, x_blocks = dW ? ((long)((N + 31) / 32) * spans + 3) / 4 : 0;
         if (w_blocks + x_blocks > 0x7FFFFFFFL) return hipErrorInvalidValue;
-        grad_operands_kernel<<<(unsigned)(w_blocks + x_blocks), 256, 0, st>>>((const uint16_t *)W, d_out, bw, (unsigned)w_blocks, (const uint8_t *)x8, sx, N, bx, d_in);
+        grad_operands_kernel<<<(unsigned)(w_blocks + x_blocks), 256, 0, st>>>((const uint16_t *)W, d_out, bw, (unsigned)w_blocks, (unsigned)parts, (const uint8_t *)x8, sx, N, bx, d_in);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         GradProduct x = {}, w = {};
