@@ -215,7 +215,7 @@ sla_status_t sla_fp8_linear_qkv(const void *x, const void *W, const void *bias, 
  *   x, W, bias, y   of the sizes and types of sla_fp8_linear; W in sla_fp8_linear_grad is that of the forward (quantised again; needed for dx only)
  *   dy    in   bf16 [N, d_out]
  *   dx    out  bf16 [N, d_in] or NULL;   dW  out  bf16 [d_out, d_in] or NULL;   db  out  bf16 [d_out] or NULL (only with dW)
- *              dW and db alone are split otherwise than beside dx: their last bits can differ
+ *              dx has the same bits with and without dW; dW and db alone are split otherwise than beside dx: their last bits can differ
  *   workspace  sla_fp8_linear_grad_workspace_bytes(N, d_in, d_out) bytes for both calls, 256-byte aligned as the checkpoint;
  *              it holds nothing from one call to the next
  * With N = 0, dW and db are set to zero (workspace, checkpoint and dy may be NULL).

@@ -440,8 +440,8 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 //       alone for all of them.  us, all and half: 1374, 1024 -> 4096 54 and 43;  10992, 1024 -> 1024 72 and 67;  10992, 384 -> 1152 44 and 38;
 //       43968, 1024 -> 1024 227 and 212;  43968, 1024 -> 4096 672 and 657;  10992, 1024 -> 4096 193 and 199.  Parts of eight and of twenty:
 //       700, 1024 -> 1024 23.5 and 19.4;  1374, 384 -> 1152 22.7 and 20.5
-//   dx  128 wide, fewer than 256 tiles: split into parts as long as those of dW and at least eight steps, where what that saves (0.27 us a step) is more than
-//       the launch and the partials of the sum cost.  us, split and whole: 197, 1024 -> 4096 24 and 43;  197, 384 -> 1152 13.2 and 15.4;
+//   dx  128 wide, fewer than 256 tiles: split into parts as long as those of dW beside it and at least eight steps, where what that saves (0.27 us a step) is
+//       more than the launch and the partials of the sum cost; alone as beside dW, so that its bits do not depend on what else is asked for.  us, split and whole: 197, 1024 -> 4096 24 and 43;  197, 384 -> 1152 13.2 and 15.4;
 //       197, 128 -> 512 11.8 and 10.3;  394, 1024 -> 1024 19.9 and 17.8;  1374, 384 -> 1152 26.2 and 22.7;  197, 4096 -> 1024 36 and 30
 struct Plan {
     bool wide;
@@ -454,10 +454,12 @@ Plan make_plan(int N, int d_in, int d_out, bool both)
     const long w256 = tiles_of(d_out, d_in, 256), x128 = tiles_of(N, d_in, 128), w128 = tiles_of(d_out, d_in, 128);
     const int x_steps = (d_out + kStepK - 1) / kStepK, w_steps = (N + kStepK - 1) / kStepK;
     p.wide = tiles_of(N, d_in, 256) >= 128 && 2 * (long)N * d_in / 65536 * d_out / kStepK >= 100 * 256;
-    p.splits_w = even_splits(w_steps, std::min((both ? 1 : 2) * (p.wide ? 128 : 256) / (p.wide ? w256 : w128), (long)w_steps / 20));
+    const long places = p.wide ? 128 : 256, w_tiles = p.wide ? w256 : w128;
+    const int beside = even_splits(w_steps, std::min(places / w_tiles, (long)w_steps / 20));         // of dW beside dx
+    p.splits_w = both ? beside : even_splits(w_steps, std::min(2 * places / w_tiles, (long)w_steps / 20));
     p.splits_x = 1;
     if (!p.wide && N && x128 < 256) {
-        const int part = std::max(8, (w_steps + p.splits_w - 1) / p.splits_w), splits = even_splits(x_steps, std::min(256 / x128, (long)x_steps / part));
+        const int part = std::max(8, (w_steps + beside - 1) / beside), splits = even_splits(x_steps, std::min(256 / x128, (long)x_steps / part));
         if (0.27 * (x_steps - x_steps / splits) > 2.5 + 0.028 * x128 * splits) p.splits_x = splits;
     }
     p.off_bx = (size_t)((d_out + 31) / 32) * 64 * d_in;
