@@ -146,9 +146,9 @@ sla_status_t sla_qk_norm_rope_grad(const sla_heads_params_t *p, const void *q, c
     if (a.norm == 0 && wanted) return fail(SLA_ERR_INVALID_ARG, "weights and biases belong to a norm; SLA_NORM_NONE has none");
     sla::HeadsGrads d = {};
     d.dw[0] = dq_weight; d.dw[1] = dk_weight; d.db[0] = dq_bias; d.db[1] = dk_bias;
-    if (empty(a)) {                      // no tokens: the gradients of the weights are zero
+    if (empty(a)) {                      // no rows: the gradients of the weights are zero
         a.N = 0;
-        if (wanted && a.H > 0) SLA_HIP(sla::launch_heads_grad(a, d, (hipStream_t)stream));
+        if (wanted && (a.H > 0 || !a.per_head)) SLA_HIP(sla::launch_heads_grad(a, d, (hipStream_t)stream));
         return SLA_OK;
     }
     if ((s = set_inputs(a, q, k, nullptr, q_weight, nullptr, k_weight, nullptr, pos)) != SLA_OK) return s;

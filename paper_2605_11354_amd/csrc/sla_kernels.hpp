@@ -137,7 +137,7 @@ struct HeadsGrads {
 // bq: 0 = bf16 outputs; 64, 128 = E4M3 with query blocks of bq tokens (64 for k and v)
 hipError_t launch_heads(const HeadsArgs &a, int bq, hipStream_t st);
 size_t heads_grad_part_bytes(int B, int H, int N, int tensors, int per_head);
-// with B N = 0 the gradients of the weights are set to zero
+// with B N = 0 the gradients of the weights are set to zero (shared ones with H = 0 too)
 hipError_t launch_heads_grad(const HeadsArgs &a, const HeadsGrads &d, hipStream_t st);
 
 }  // namespace sla
