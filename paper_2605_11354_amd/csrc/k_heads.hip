@@ -158,6 +158,7 @@ __device__ __forceinline__ void make_table(const HeadsArgs &a, int valid, Row po
     lds_barrier();
 }
 
+// `otherwise` where there are none: 1 and -0, which keep the sign of a zero
 __device__ __forceinline__ void load_weights(const float *p, int head, int per_head, int o, float otherwise, float (&w)[8])
 {
 #pragma unroll
@@ -223,7 +224,7 @@ __global__ __launch_bounds__(256, 4) void heads_kernel(HeadsArgs a)
                 it = item_of(a, unit + k / kOct);
                 if (it.tensor < 2 && (a.per_head || it.tensor != have)) {
                     load_weights(a.w[it.tensor], it.head, a.per_head, o, 1.f, w);
-                    load_weights(a.b[it.tensor], it.head, a.per_head, o, 0.f, bias);
+                    load_weights(a.b[it.tensor], it.head, a.per_head, o, -0.f, bias);
                     have = it.tensor;
                 }
             }
@@ -285,7 +286,7 @@ __global__ __launch_bounds__(256, 3) void heads_e4m3_kernel(HeadsArgs a)
             float w[8], bias[8];
             if (it.tensor < 2) {
                 load_weights(a.w[it.tensor], it.head, a.per_head, o, 1.f, w);
-                load_weights(a.b[it.tensor], it.head, a.per_head, o, 0.f, bias);
+                load_weights(a.b[it.tensor], it.head, a.per_head, o, -0.f, bias);
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
