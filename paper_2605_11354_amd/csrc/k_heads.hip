@@ -13,7 +13,7 @@
 // sines of those tokens are computed once, into LDS, for all heads and both tensors.
 // HBM bound: 2 bytes in, 2 (E4M3: 1) out per element; backward 4 in, 2 out.  At the copy rate a CU has twenty vector instructions
 // for an element, so each is counted: the root is v_rsq_f32 (one unit in the last place), rotation is a product and a
-// multiply-add with a cross-lane operand (the table holds the sines with both signs), the E4M3 codes come from a product with 1 / scale.
+// multiply-add with a cross-lane operand (the table holds the sines with both signs), the E4M3 codes come from the three steps of BlockDivisor.
 // Measured, layer norm and two axes: 43968 tokens of 16 heads, q, k and v: bf16 118 us (540 MB, 4.6 TB/s), E4M3 93 us with 64-row query blocks
 // (405 MB, 4.3 TB/s) and 109 with 128-row ones; 10992 tokens bf16 30 us (4.5 TB/s); gradients of 13814 tokens of 12 heads with weights of each head 45 us
 // (170 MB, 3.8 TB/s) and 4 for the sums; 32 tokens of 16 heads 4.6 us, a launch and three trips to memory.
@@ -247,7 +247,9 @@ __global__ __launch_bounds__(256, 4) void heads_kernel(HeadsArgs a)
 // item.  With SUB = 2 two waves share an item, each with its half of the query block, and exchange the block's maximum through LDS.
 // On 43968 tokens of 16 heads that exchange costs 6 of 109 us, the angles 10, norm and rotation another 10 that do not hide behind the copies (all three
 // left out: 88; the 64-row form 93, and 86).
-// The codes are those of y in fp32: rounded once, to E4M3.  v takes the exact quotient, as the stand-alone quantiser does.
+// The codes are those of the fp32 quotient y / scale, as with the stand-alone quantiser: rounded once, to E4M3.  The scale of q and k can have any significand;
+// for all 2^23 of them the three-step quotient is the division's wherever it lies within six units of a border between two codes (gone
+// through on the host; tests/test_division_step_any_scale.py has a selection), and elsewhere a unit in its last place does not matter.
 template <int ROT, int SUB>
 __global__ __launch_bounds__(256, 3) void heads_e4m3_kernel(HeadsArgs a)
 {
@@ -321,15 +323,8 @@ __global__ __launch_bounds__(256, 3) void heads_e4m3_kernel(HeadsArgs a)
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             if (8 * k >= mine) continue;
-            if (it.tensor < 2) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[k][e] *= divide.y;
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[k][e] = divide(y[k][e]);
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[k][e] = __builtin_amdgcn_fmed3f(y[k][e], -448.0f, 448.0f);       // NaN gives -448, as with the stand-alone quantiser
+            for (int e = 0; e < 8; ++e) y[k][e] = __builtin_amdgcn_fmed3f(divide(y[k][e]), -448.0f, 448.0f);       // NaN gives -448, as with the stand-alone quantiser
             if (r0 + 8 * k < mine)
                 *(uint2 *)(out + out_off[row0 + 8 * k]) = make_uint2(pack_e4m3(y[k][0], y[k][1], y[k][2], y[k][3]), pack_e4m3(y[k][4], y[k][5], y[k][6], y[k][7]));
         }
