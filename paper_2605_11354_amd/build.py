@@ -17,10 +17,10 @@ PROBED = ["k_attend.hip", "k_linear.hip", "k_classify.hip"]
 SOURCES = ["sla_api.hip", "k_classify.hip", "k_states.hip", "k_aggregate.hip", "k_attend.hip", "k_attend_short.hip", "k_backward.hip", "k_quant.hip", "k_linear.hip",
            "k_linear_grad.hip", "mxfp4_api.hip", "k_mxfp4.hip", "heads_api.hip", "k_heads.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-ffp-contract=off", "-Wall", "-Wextra",
-         "-Wno-unused-parameter", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-         "-mllvm", "-amdgpu-mfma-vgpr-form=1"]   # MFMA accumulators stay in VGPRs: no AGPR copy traffic
+         "-Wno-unused-parameter", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
+VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]   # MFMA accumulators stay in VGPRs: no AGPR copy traffic
 # The wide tiles of these files hold 256 accumulators a lane, which only the other half of the register file has room for (with
-# the flag its main loop copies two hundred registers a step)
+# VGPR_FORM its main loop copies two hundred registers a step)
 AGPR_FORM = ["k_linear_grad.hip", "k_mxfp4.hip"]
 
 
@@ -31,11 +31,14 @@ def _hipcc() -> str:
     return "hipcc"
 
 
+def flags_of(src: str) -> list:
+    return FLAGS if src in AGPR_FORM else FLAGS + VGPR_FORM
+
+
 def _compile(job) -> str:
     src, probe = job if isinstance(job, tuple) else (job, False)
     obj = os.path.join(OBJ, ("probe_" if probe else "") + src.replace(".hip", ".o"))
-    flags = FLAGS[:-2] if src in AGPR_FORM else FLAGS
-    cmd = [_hipcc(), *flags, *(["-DSLA_PROBE_TIME"] if probe else []), "-c", os.path.join(CSRC, src), "-o", obj]
+    cmd = [_hipcc(), *flags_of(src), *(["-DSLA_PROBE_TIME"] if probe else []), "-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     err = "\n".join(l for l in r.stderr.splitlines() if "packed-fp32-ops" not in l)
     if r.returncode != 0:
