@@ -157,11 +157,12 @@ __global__ __launch_bounds__(256, 2) void fp8_gemm_kernel(const uint8_t *__restr
     // channel tile fastest: the workgroups that share a token tile run side by side on one XCD, so the activations come from HBM
     // once and the weight matrix stays in every XCD's L2.  A weight matrix of 3 MB or more does not stay there, and where one token tile has twenty-four channel
     // tiles or more it is read again for every two token tiles: large launches then take eight token tiles through all channel tiles, token tile
-    // fastest, so that the sixty-four workgroups on an XCD share eight and eight (3 MB for K = 1024).  Up to K = 2048: longer rows of eight token tiles
-    // do not stay in the L2 either, and come from HBM again for every eight channel tiles.  us with the quantiser, by channel tiles and by eights:
+    // fastest, so that the sixty-four workgroups on an XCD share eight and eight (3 MB for K = 1024).  Longer rows than K = 2048 do
+    // not stay in the L2 as a whole: what eight token tiles share they then share only if they start at the same K step (below), that is where the channel tiles
+    // are a multiple of K / 128.  us with the quantiser, by channel tiles and by eights:
     //     43968 tokens, K = 1024: 24 channel tiles 194.7, 189.3;  28: 210.6, 210.4;  32: 239.5, 228.6;  64: 437.3, 421.9;  12: 109.0, 107.9;  9: 87.5, 90.2
     //     K = 2048: 24: 330.2, 323.1;  32: 420.9, 401.0;  18: 262.5, 265.3;  9: 162.8, 166.1      K = 512: 24: 115.2, 114.9;  48: 214.9, 201.7;  16: 75.8, 78.6
-    //     K = 4096: 24: 648.7, 655.5;  32: 807.8, 789.3;  36: 812.2, 897.7;  9: 332.7, 357.9      K = 8192: 32: 1583, 1575;  36: 1564, 2096;  18: 1051, 1209
+    //     K = 4096: 24: 648.7, 655.5;  32: 807.8, 789.3;  36: 812.2, 897.7;  64: 1331.6, 1284.8;  9: 332.7, 357.9      K = 8192: 32: 1583, 1575;  36: 1564, 2096;  64: 2522, 2520
     //     10992 tokens, K = 512: 16: 28.4, 31.6;  33: 42.3, 43.1;  48: 61.1, 59.2      K = 1024: 16: 39.7, 41.6;  24: 57.6, 56.7;  32: 69.3, 65.4
     const int item = (int)xcd_remap(blockIdx.x, total);
     if (item >= total) return;
@@ -170,7 +171,7 @@ __global__ __launch_bounds__(256, 2) void fp8_gemm_kernel(const uint8_t *__restr
 #endif
     SLA_GT(0);
     int it = (int)((unsigned)item / (unsigned)n_ot), ot = item - it * n_ot;
-    if (TB == 4 && n_ot >= 24 && K <= 2048 && n_ot * K >= 24 * 1024) {
+    if (TB == 4 && n_ot >= 24 && n_ot * K >= 24 * 1024 && (K <= 2048 || n_ot % (K / 128) == 0)) {
         const int first = (it & ~7), in = item - first * n_ot, rows = min(8, (M + kTok - 1) / kTok - first);
         ot = (int)((unsigned)in / (unsigned)rows);
         it = first + in - ot * rows;

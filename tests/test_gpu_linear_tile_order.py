@@ -1,5 +1,5 @@
 """The FP8 layer's large tiles on both sides of the sizes at which they are taken in another order (24 channel tiles of 128, rows of 2048
-elements, 3 MB of weights): every row right, and the same bits twice.
+elements, 3 MB of weights; longer rows: channel tiles a multiple of K / 128): every row right, and the same bits twice.
 
 The products of the codes are exact and K of them are summed in fp32: an output is off by at most (K + 4) 2^-24 of the sum of magnitudes
 (the sum, two scales, the bias), before half a bf16 step, 2^-8 relative."""
@@ -19,7 +19,7 @@ def quantised(x):
     return (x / scale).clamp(-448.0, 448.0).to(torch.float8_e4m3fn).double() * scale.double()
 
 
-@pytest.mark.parametrize("N,d_in,d_out", [(10992, 1024, 2944), (10992, 1024, 2952), (10992, 2048, 3080), (10992, 2176, 3080), (8200, 896, 3200), (5000, 512, 6144), (4097, 512, 6152), (25601, 256, 1160)])
+@pytest.mark.parametrize("N,d_in,d_out", [(10992, 1024, 2944), (10992, 1024, 2952), (10992, 2048, 3080), (10992, 2176, 3080), (4100, 4096, 4096), (4100, 4096, 4104), (8200, 896, 3200), (5000, 512, 6144), (4097, 512, 6152), (25601, 256, 1160)])
 def test_every_tile_is_right(N, d_in, d_out):
     g = torch.Generator(device="cuda").manual_seed(d_in + d_out)
     x = torch.randn((N, d_in), generator=g, device="cuda").mul_(torch.exp(torch.randn((N, 1), generator=g, device="cuda"))).to(torch.bfloat16)
