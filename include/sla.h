@@ -207,8 +207,9 @@ sla_status_t sla_fp8_linear_qkv(const void *x, const void *W, const void *bias, 
  * y as sla_fp8_linear does and leaves the E4M3 codes and the scales of x, which it multiplies anyway, in `checkpoint`:
  * sla_fp8_checkpoint_bytes(N, d_in), about N (d_in + 4) bytes, half of x; x itself is not needed again.  Its scales are
  * max(amax, 1e-8) * fp32(1 / 448), what PyTorch on the GPU makes of the formula amax / 448.0, so that its codes are those of the
- * fake-quantised layer as one writes it there; sla_fp8_linear divides: where x / scale lies half-way between two codes, the two can
- * choose different ones.
+ * fake-quantised layer as one writes it there; sla_fp8_linear and sla_fp8_linear_qkv divide: where x / scale lies half-way between two codes, the
+ * two rules can choose different ones (0.07 % of the codes of random bf16 values, up to 6 % of a row; the two y are 3e-3 apart in the
+ * 2-norm, of which their stores alone make up to 2.3e-3).  To serve a model with the very numbers that it was trained with, call sla_fp8_linear_save there too.
  * sla_fp8_linear_grad takes them for the gradients
  *     dx = dy W_q     dW = dy^T x_q     db = sum over tokens of dy        x_q, W_q = bf16(code * scale)
  * with products summed in fp32 in a fixed order (no atomics: the same inputs give the same bits) and rounded once to bf16.
@@ -216,8 +217,8 @@ sla_status_t sla_fp8_linear_qkv(const void *x, const void *W, const void *bias, 
  *   dy    in   bf16 [N, d_out]
  *   dx    out  bf16 [N, d_in] or NULL;   dW  out  bf16 [d_out, d_in] or NULL;   db  out  bf16 [d_out] or NULL (only with dW)
  *              dx has the same bits with and without dW; dW and db alone are split otherwise than beside dx: their last bits can differ
- *   workspace  sla_fp8_linear_grad_workspace_bytes(N, d_in, d_out) bytes for both calls, 256-byte aligned as the checkpoint;
- *              it holds nothing from one call to the next
+ *   workspace  sla_fp8_linear_grad_workspace_bytes(N, d_in, d_out) bytes for both calls (one buffer of the largest size serves all layers of
+ *              a stream, in both directions), 256-byte aligned as the checkpoint; it holds nothing from one call to the next
  * With N = 0, dW and db are set to zero (workspace, checkpoint and dy may be NULL).
  * sla_fp8_checkpoint_restore writes x_q [N, d_in], bf16, for what else of a backward pass needs the layer's input.
  */
@@ -250,7 +251,8 @@ sla_status_t sla_dequantise_mxfp4(const void *codes, const void *scales, int64_t
  *   bias   in   bf16 [d_out] or NULL
  *   y      out  bf16 [N, d_out]
  *   workspace  sla_mxfp4_linear_workspace_bytes(N, d_in, d_out) bytes (may be 0: then NULL will do), 256-byte aligned
- * A token with an infinity or NaN, or one that meets a weight block with s = 255, comes out NaN; others are not affected.
+ * All channels of a token with an infinity or NaN, and a channel with a weight block of s = 255 for all tokens, come out NaN; other
+ * values are not affected.
  */
 sla_status_t sla_mxfp4_linear_workspace_bytes(int32_t N, int32_t d_in, int32_t d_out, size_t *bytes);
 sla_status_t sla_mxfp4_linear(const void *x, const void *W_codes, const void *W_scales, const void *bias, int32_t N, int32_t d_in,
@@ -260,19 +262,20 @@ sla_status_t sla_mxfp4_linear(const void *x, const void *W_codes, const void *W_
  * Norm of every head's queries and keys and position rotation, in one pass from a projection's output to the form the
  * attention takes its inputs in.  For every token and head, over the 64 channels of its row x of q (and of k):
  *     u = (x - m) r,  r = 1 / sqrt(mean((x - m)^2) + eps)      m = mean(x) (SLA_NORM_LAYER), 0 (SLA_NORM_RMS)
- *     n = u * weight + bias                                    (SLA_NORM_NONE: n = x)
+ *     n = u * weight + bias                                    (SLA_NORM_NONE: n = x; without rotation every bit of a number)
  *     y_i = n_i cos a - n_p sin a,   y_p = n_p cos a + n_i sin a      for each pair (i, p) of channels
  * Rotation: axes = 1: one position per token turns all 64 channels, pair j = 0 .. 31 by a = position * base^(-j / 32);
  * axes = 2: two positions (row and column of a patch) turn channels 0 .. 31 and 32 .. 63, pair j = 0 .. 15 of each half by
  * a = position * base^(-j / 16); axes = 0: none.  The pairs of a span of S channels are (j, j + S/2) (SLA_PAIR_HALVES)
- * or (2j, 2j + 1) (SLA_PAIR_ADJACENT).  Angles are reduced in 64 bits: any int32 position is as exact as a small one.
+ * or (2j, 2j + 1) (SLA_PAIR_ADJACENT).  Angles are reduced in 64 bits: cosines and sines are off by at most 1e-7 for positions of
+ * magnitudes below 2^28 and by 4e-7 up to the ends of int32.
  * v rows are brought into the output layout (and data type) unchanged.
  */
 typedef enum { SLA_NORM_NONE = 0, SLA_NORM_RMS = 1, SLA_NORM_LAYER = 2 } sla_norm_t;
 typedef enum { SLA_PAIR_HALVES = 0, SLA_PAIR_ADJACENT = 1 } sla_pairing_t;
 
 typedef struct {
-    int32_t B, H, N, D;          /* batch, heads, tokens per item, head dim (must be 64) */
+    int32_t B, H, N, D;          /* batch, heads, tokens per item, head dim (must be 64); B H at most 65535, as in sla_forward */
     int32_t norm;                /* sla_norm_t */
     int32_t norm_per_head;       /* weights and biases: 0: [D]; 1: [H, D] */
     int32_t axes;                /* positions per token: 0 (no rotation), 1 or 2 */
@@ -299,7 +302,8 @@ sla_status_t sla_qk_norm_rope(const sla_heads_params_t *p, const void *q, const 
 /*
  * The same with the outputs in the E4M3 form that sla_forward takes: codes in `layout` and block scales as
  * sla_quantise_e4m3 defines them (blk = bq for Q, 64 for K and V; scale = max(amax, 1e-8) / 448), of the values y before any
- * rounding to bf16: one rounding, to E4M3.  V comes out as sla_quantise_e4m3 would leave it, bit for bit.
+ * rounding to bf16: one rounding, to E4M3.  V, and without norm and rotation Q and K too, come out as sla_quantise_e4m3 would leave
+ * them, bit for bit.
  *   Q8, K8, V8  out  uint8;   sQ  out  fp32 [B,H,ceil(N/bq)];   sK, sV  out  fp32 [B,H,ceil(N/64)]
  */
 sla_status_t sla_qk_norm_rope_e4m3(const sla_heads_params_t *p, const void *q, const void *k, const void *v,

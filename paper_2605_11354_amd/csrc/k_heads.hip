@@ -14,9 +14,9 @@
 // HBM bound: 2 bytes in, 2 (E4M3: 1) out per element; backward 4 in, 2 out.  At the copy rate a CU has twenty vector instructions
 // for an element, so each is counted: the root is v_rsq_f32 (one unit in the last place), rotation is a product and a
 // multiply-add with a cross-lane operand (the table holds the sines with both signs), the E4M3 codes come from the three steps of BlockDivisor.
-// Measured, layer norm and two axes: 43968 tokens of 16 heads, q, k and v: bf16 118 us (540 MB, 4.6 TB/s), E4M3 93 us with 64-row query blocks
-// (405 MB, 4.3 TB/s) and 109 with 128-row ones; 10992 tokens bf16 30 us (4.5 TB/s); gradients of 13814 tokens of 12 heads with weights of each head 45 us
-// (170 MB, 3.8 TB/s) and 4 for the sums; 32 tokens of 16 heads 4.6 us, a launch and three trips to memory.
+// Measured, layer norm and two axes, in a stream of calls: 43968 tokens of 16 heads, q, k and v: bf16 110 to 118 us (540 MB, 4.6 to 4.9 TB/s), E4M3 96 us with
+// 64-row query blocks (405 MB, 4.2 TB/s) and 110 to 115 with 128-row ones; 10992 tokens bf16 28 to 30 us (4.5 to 4.8 TB/s); gradients of 13814 tokens of 12 heads
+// with weights of each head 45 us (170 MB, 3.8 TB/s) and 4 to 5 for the sums; 32 tokens of 16 heads 4.6 us, a launch and three trips to memory.
 #include "sla_common.hpp"
 #include "sla_kernels.hpp"
 
@@ -245,8 +245,8 @@ __global__ __launch_bounds__(256, 4) void heads_kernel(HeadsArgs a)
 
 // E4M3 outputs with query blocks of 64 SUB tokens; a workgroup takes 64 SUB tokens of one sequence, a unit is 64 tokens of one
 // item.  With SUB = 2 two waves share an item, each with its half of the query block, and exchange the block's maximum through LDS.
-// On 43968 tokens of 16 heads that exchange costs 6 of 109 us, the angles 10, norm and rotation another 10 that do not hide behind the copies (all three
-// left out: 88; the 64-row form 93, and 86).
+// On 43968 tokens of 16 heads norm, rotation and their angles take 18 of 112 us that do not hide behind the copies, in the 64-row form, without the
+// exchange, 5 of 96 (called without norm and rotation: 93 and 90).
 // The codes are those of the fp32 quotient y / scale, as with the stand-alone quantiser: rounded once, to E4M3.  The scale of q and k can have any significand;
 // for all 2^23 of them the three-step quotient is the division's wherever it lies within six units of a border between two codes (gone
 // through on the host; tests/test_division_step_any_scale.py has a selection), and elsewhere a unit in its last place does not matter.
@@ -474,11 +474,15 @@ __global__ __launch_bounds__(1024) void heads_grad_reduce_kernel(const float *__
 
 namespace {
 // Workgroups: the items of a block of tokens are split over several; each computes the block's angles anew.
-// bf16 and gradients: into 4096 workgroups or what the items give (43968 tokens of 16 heads: 128 us with 1374 workgroups, 118 with 2748,
-// 111 with 4122, 113 with 8244; 10992 tokens 43, 36, 36, 37).
+// bf16 and gradients: into 4096 workgroups or what the items give.  us, by workgroups of a block of tokens, the rule's in brackets: bf16, 43968 tokens
+// of 16 heads 1: 118, 2: 127, 4: 118, [6]: 110, 12: 113;  8 x 1374 tokens 1: 27, 2: 33, [3]: 28;  gradients with weights of each head, 2 x 6907 tokens of 12 heads
+// 1: 59, 2: 53, 3: 41.5, 4: 41.6, 6: 46, [9]: 44;  43968 tokens of 16 heads 1: 159, 2: 178, [6]: 160, 12: 165;  1374 tokens 1: 72, 6: 22, [12]: 16;  with shared
+// weights 2 x 6907 tokens 1: 39, 2: 54, [3]: 45;  43968 1: 157, [6]: 164, 12: 182;  1374 1: 25, [3]: 16.  So gradients of middle sizes lose up to 6 % by
+// it, with shared weights 14 %; no one number of workgroups suits them all.
 // E4M3: a CU holds three workgroups, and the angles of 128 tokens cost as much as four items, so whole rounds of 768 count: the
-// number of parts with the shortest rounds (43968 tokens, 128-row blocks: 344 workgroups 132 us, 688 112, 1032 120, 2064 107;
-// 8 x 1374 tokens, 64-row blocks: 176 41, 704 32, 1056 36).
+// number of parts with the shortest rounds.  43968 tokens of 16 heads, 128-row blocks 1: 130, [2]: 110, 3: 117, 4: 112, 6: 106, 12: 110;  64-row blocks [1]: 95,
+// 2: 105, 3: 97, 6: 96;  8 x 1374 tokens, 64-row 1: 47, 2: 37, [4]: 29.5, 6: 30.7, 128-row 4: 42, [8]: 32.5, 12: 35;  10992 tokens of 12 heads, 128-row 3: 40,
+// [6]: 29.5, 9: 31;  137400 tokens 1: 311, [2]: 305, 3: 281, 4: 295, 6: 281: where there are several rounds either way it gives up 4 to 8 %.
 void split_items(HeadsArgs &a, long blocks, int at_once, bool rounds)
 {
     const int items = a.tensors * a.H, most = (items + at_once - 1) / at_once;

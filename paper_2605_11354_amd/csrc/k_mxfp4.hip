@@ -109,7 +109,7 @@ __global__ __launch_bounds__(256) void dequantise_mxfp4_kernel(const uint32_t *_
 // deep); the operands of a part are read while the products of the one before run, and reads and copies stand between the products,
 // because a wave of the largest tile is alone on its SIMD.  The one barrier of a step stands before the products of its second part,
 // whose operands are in registers by then.
-// Measured: 43968 tokens, 4096 -> 1024 106 us (3.5 PFLOP/s).
+// Measured: 43968 tokens, 4096 -> 1024 107 us in a stream of passes (3.5 PFLOP/s), 114 to 130 from rest.
 // D[channel][token] (W is the first operand): a lane's four consecutive registers are consecutive channels.
 template <int TM, int TN>
 __global__ __launch_bounds__(256, TM == 4 ? 1 : 2) void mxfp4_gemm_kernel(const uint8_t *__restrict__ A, const uint8_t *__restrict__ As, const uint8_t *__restrict__ W,
@@ -432,8 +432,8 @@ bool mxfp4_turns_weights(int M, int O) { return M >= 2L * O; }
 
 // Tiles.  64 x 128 while each has a CU of its own (256 of them, 2048 x 1024 -> 1024: 6.1 us, 6.7 with 128 x 128; 352, 700 x 1024 -> 4096: 7.5 and
 // 7.0, from 4096 channels 23.3 and 17.0).  A 256 x 256 tile reads half as much from LDS and L2 for a product as four of 128 x 128, but has a CU to
-// itself, with nothing under its start and end: from 192 on (172, 10992 x 1024 -> 1024: 15.2 us and 12.9; 192, 3000 x 1024 -> 4096: 16.0 and 14.0,
-// x 4096: 34.8 and 41.0; 2752, 43968 x 1024 -> 4096: 150 and 154; 688, 43968 x 4096 -> 1024: 102 and 108).
+// itself, with nothing under its start and end: from 192 on, whatever K is, which loses on short rows there (us, 256 x 256 and 128 x 128: 172,
+// 10992 x 1024 -> 1024: 15.2 and 12.9; 192, 3000 x 1024 -> 4096: 16.0 and 14.0, x 4096: 34.8 and 41.0; 2752, 43968 x 1024 -> 4096: 150 and 154; 688, 43968 x 4096 -> 1024: 102 and 108).
 hipError_t launch_mxfp4_gemm(const void *A, const void *As, const void *W, const void *Ws, bool by_steps, const void *bias, int M, int O, int K, void *Y, hipStream_t st)
 {
     const long wide = (long)((M + 255) / 256) * ((O + 255) / 256), narrow = (long)((M + 63) / 64) * ((O + 127) / 128);

@@ -119,9 +119,10 @@ __device__ __forceinline__ bf16x8 pack8(const f32x16 &a, int base)
 
 // x / scale for many x and one block scale = max(amax, 1e-8) / 448 of bf16 values, with the bits of the IEEE division:
 // y = RN(1 / d) once (a true division), then q = RN(x y), r = d q - x (exact in one fma), RN(q - r y) is the correctly
-// rounded quotient (Markstein's division step; written with this sign of r, a zero quotient keeps the sign of x).  It needs y correctly rounded and fails only for a significand of d of all
+// rounded quotient (Markstein's division step; written with this sign of r, a zero quotient keeps the sign of x).  It needs y correctly rounded and can fail only for a significand of d of all
 // ones, which no such scale has: amax is m 2^e with m below 256, m / 7 differs from every power of two by a part in 256 or
-// is equal to it, and 1e-8 / 448 is one number (tests/test_division_step.py goes through all of them).  Quotients are at
+// is equal to it, and 1e-8 / 448 is one number (tests/test_division_step.py goes through all of them).  The scales of normed and rotated heads can have any
+// significand; the codes are those of the division for all of them (heads_e4m3_kernel).  Quotients are at
 // most 448 in magnitude and anything below 2^-10 becomes the code 0, so the exponent range plays no part for a finite scale.
 // Three instructions per element instead of the ten of the division's expansion.
 // An infinite scale: x / inf is a zero of x's sign, and NaN for an infinite x.  d = 0 and y = 0 give just that

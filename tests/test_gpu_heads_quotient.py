@@ -59,3 +59,16 @@ def test_rotation_by_nothing(axes, pairing, bq):
         torch.cuda.synchronize()
         assert torch.equal(s, want[1])
         assert torch.equal(c.view(torch.float8_e4m3fn).float(), want[0].view(torch.float8_e4m3fn).float())
+
+
+@pytest.mark.parametrize("bq", [64, 128])
+def test_infinities_and_nan(bq):
+    q, k, v = inputs(2, 300, 3)
+    for t in (q, k, v):
+        t[0, 5, 0, 7], t[1, 70, 1, 0], t[1, 299, 2, 63] = float("inf"), float("nan"), float("-inf")
+        t[0, 128:192, 2] = float("nan")
+    codes, scales = run(B.make_heads_params(q, norm="none", axes=0), (q, k, v), bq, "bhnd")
+    for c, s, x, blk in zip(codes, scales, (q, k, v), (bq, 64, 64)):
+        want = quantiser(x, blk, "bhnd")
+        torch.cuda.synchronize()
+        assert torch.equal(s, want[1]) and torch.equal(c, want[0])
