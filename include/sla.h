@@ -285,8 +285,8 @@ typedef struct {
     float   eps;                 /* a normal fp32 number > 0 unless SLA_NORM_NONE; the squares are summed in fp32, so |x| must stay below 2^60 */
     double  base;                /* >= 1, finite; ignored with axes = 0 */
     int64_t batch_stride, token_stride, head_stride;
-                                 /* elements between the rows of q, k, v (and of dq, dk, dv): multiples of 8, at least 64, in any order, and
-                                    no two rows overlap.  A fused projection [B,N,3,H,64]: N 3 H 64, 3 H 64, 64 */
+                                 /* elements between the rows of q, k, v (and of dq, dk, dv): multiples of 8, at least 64, in any order, each
+                                    (from the smallest on) at least what the smaller ones reach over: rows neither overlap nor interleave.  A fused projection [B,N,3,H,64]: N 3 H 64, 3 H 64, 64 */
 } sla_heads_params_t;
 
 /*
